@@ -329,6 +329,46 @@ TDP_API int tdp_probe_mfma_bf16(int32_t iters, int32_t launches, int32_t random_
 TDP_API int tdp_stage_timing_enable(tdp_stage* st, int32_t on);
 TDP_API int tdp_stage_timing_read(tdp_stage* st, float* ms /* host [8] */);
 
+/* ---- projections in 8-bit integers -----------------------------------------------------------------
+ * y = x W with both held as 8-bit integers, a scale for each row of x (token) and each column of W (output
+ * channel), and exact sums: half the bytes of a bf16 projection to stream (what bounds a decode step's projections,
+ * Sec. 3.4) and twice its matrix rate.  A vector v is held as codes c and a scale: with a = max |v| the scale is a / 127
+ * and c = rint(v * (127 / a)), each operation rounded in fp32; an element is off by at most half a scale.
+ *   y[m][n] = scale_x[m] * scale_w[n] * sum_k c_x[m][k] c_w[k][n]
+ * The sum is a whole number, so a row's result does not depend on the other rows of the call.  A row or column that holds an
+ * infinity or a NaN has scale NaN, and with it its whole result; one of zeros has scale 0.
+ * A tdp_linear_i8 owns the codes and scales of one weight matrix and scratch for max_rows rows.  It lives on the
+ * device that is current when it is created, and calls on it need that device current.  Like a stage it must not be driven from two
+ * streams at once, nor by two captured graphs that replay at once. */
+typedef struct tdp_linear_i8 tdp_linear_i8;
+typedef struct {
+  int32_t in_features;   /* K: a multiple of 8, at most 131072 */
+  int32_t out_features;  /* N: a multiple of 4; gated: of 8 */
+  int32_t gated;         /* 1: W = [W_gate | W_up] side by side, as in tdp_gemm_bf16: the result has N / 2 columns */
+  int32_t max_rows;      /* rows per call */
+} tdp_linear_i8_config;
+TDP_API int tdp_linear_i8_create(const tdp_linear_i8_config* cfg, tdp_linear_i8** out);
+TDP_API void tdp_linear_i8_destroy(tdp_linear_i8* h);
+/* W row-major [K, N], host or device, fp32 or bf16: quantised column by column and laid out.  Synchronous. */
+TDP_API int tdp_linear_i8_set_weight(tdp_linear_i8* h, const void* src, int32_t dtype, int32_t mem, int64_t rows, int64_t cols);
+/* A matrix that is quantised already: codes int8 row-major [K, N] and fp32 scales [N], both where mem says.  Synchronous. */
+TDP_API int tdp_linear_i8_set_codes(tdp_linear_i8* h, const int8_t* codes, const float* scales, int32_t mem, int64_t rows, int64_t cols);
+/* Added to every row of an ungated result: [N], fp32 or bf16.  Synchronous. */
+TDP_API int tdp_linear_i8_set_bias(tdp_linear_i8* h, const void* src, int32_t dtype, int32_t mem, int64_t n);
+/* Tuning and tests: the following calls make the product in exactly one way, tile = a tile number of tdp_gemm_plan (not the one that is
+ * made for chunked sums), splits = the split-K factor (over k-tiles of 128, none of them empty); tile = 0: planned, the default.  A call whose
+ * partials exceed the workspace (8 * min(max_rows, 512) * N, N rounded up to 256, at most 64 Mi) is then TDP_EINVAL.  Results are the same
+ * to the bit. */
+TDP_API int tdp_linear_i8_set_form(tdp_linear_i8* h, int32_t tile, int32_t splits);
+/* out[m] = y[m] (+ bias) (+ residual[m]), or silu(gate) * up if gated, for M <= max_rows rows (M = 0: nothing to do).
+ *   x          dev, x_dtype, rows ld_x elements apart, 16-byte aligned: quantised by the call
+ *   residual   dev, out_dtype, rows ld_residual elements apart, or null; gated: null.  May be out itself
+ *   out        dev, out_dtype, rows ld_out elements apart: [M][N], gated [M][N / 2]; columns behind those are left as they are
+ * TDP_F32 or TDP_BF16 each; out and residual aligned to four elements, row by row.  Sums, scales, bias and residual are joined in fp32
+ * and rounded once. */
+TDP_API int tdp_linear_i8_run(tdp_linear_i8* h, const void* x, int32_t x_dtype, int64_t ld_x, int32_t M, const void* residual,
+                              int64_t ld_residual, void* out, int32_t out_dtype, int64_t ld_out, void* stream);
+
 /* ---- the two ends of the pipeline ---------------------------------------------------------------
  * What runs in front of the first stage and behind the last one so that a chain of stages turns
  * token ids into token ids (the paper measures generated tokens per second on whole models, Sec.
@@ -345,6 +385,8 @@ typedef struct {
 #define TDP_E_EMBEDDING 0  /* [vocab_size, d_model] */
 #define TDP_E_FINAL_NORM 1 /* [d_model, 1] */
 #define TDP_E_LM_HEAD 2    /* [d_model, vocab_size] row-major ([in, out] like every projection) */
+#define TDP_E_LM_HEAD_I8 3 /* the same, held in 8-bit integers with a scale for each token of the vocabulary (see tdp_linear_i8); the
+                              rows are then quantised behind the final norm.  The projection is in the form that was set last. */
 TDP_API int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out);
 TDP_API void tdp_ends_destroy(tdp_ends* e);
 /* src: host or device (mem), fp32 or bf16 (dtype); synchronous */
@@ -364,6 +406,29 @@ TDP_API int tdp_lm_head(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, c
 /* Greedy selection alone: out[m] = lowest index among the maxima of logits[m][0..n), rows ld apart.
  * All device pointers.  NaN entries never win; a row of NaNs gives 0. */
 TDP_API int tdp_argmax_rows(const float* logits, int32_t M, int32_t n, int64_t ld, int32_t* out, void* stream);
+
+/* Log-probabilities of given logits: for every row m of [M][n] logits (dev, TDP_F32 or TDP_BF16, rows ld >= n elements apart, at any
+ * alignment of their type; n up to 2^30)
+ *   logprob[m]     ln p of token targets[m] (dev int32 [M]); a target outside [0, n), such as -1 for none, has minus infinity.
+ *                  targets null: of the row's largest logit
+ *   entropy[m]     - sum p ln p, in nats
+ *   top_index[m][j], top_logprob[m][j], j < n_top: the likeliest tokens in order, of equal ones the lower index first (dev int32 / fp32
+ *                  [M][n_top]); n_top 0 .. TDP_MAX_TOP, at most n
+ * with p = softmax of the row.  logprob and entropy may be null, and top_index and top_logprob with n_top = 0.  Logits of minus infinity are
+ * tokens of probability 0.  A row with a NaN or plus infinity, or with nothing but minus infinity, has no distribution: its logprob
+ * (but for targets outside), entropy and top_logprob are NaN; top_index still orders its logits, without the NaN, and is -1 behind
+ * the last.  Sums are fp32, relative to the row's maximum. */
+#define TDP_MAX_TOP 32
+TDP_API int tdp_logprob_rows(const void* logits, int32_t dtype, int32_t M, int32_t n, int64_t ld, const int32_t* targets, int32_t n_top,
+                             float* logprob, float* entropy, int32_t* top_index, float* top_logprob, void* stream);
+/* The same behind tdp_lm_head's norm and projection (hidden_in, n_rows_in, row_index, M as there), with the greedy token as
+ * there in next_token (dev int32 [M] or null): what an engine answers a token with, or, with a prompt's own next tokens as targets, what
+ * scores it.  Logits are kept inside, and where neither next_token nor n_top asks for tokens they are not stored at all.  An ends
+ * object must not be driven from two streams at once, nor by two captured graphs that replay at once; this call needs the device
+ * current on which it was created. */
+TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int32_t* row_index, int32_t M,
+                                 const int32_t* targets, int32_t n_top, int32_t* next_token, float* logprob, float* entropy,
+                                 int32_t* top_index, float* top_logprob, void* stream);
 
 #ifdef __cplusplus
 }

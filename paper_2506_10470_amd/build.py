@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtdp.so")
 SCHED_LIB = os.path.join(HERE, "libtdp_sched.so")
-SOURCES = ("gemm.hip", "attention.hip", "elementwise.hip", "stage.hip", "probe.hip", "gemm_static.hip")
+SOURCES = ("gemm.hip", "gemm_int.hip", "gemm_stats.hip", "attention.hip", "elementwise.hip", "stage.hip", "probe.hip",
+           "gemm_static.hip", "linear_i8.hip", "logprob.hip")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
@@ -41,7 +42,7 @@ def build(verbose: bool = False) -> str:
         obj = os.path.join(BUILD, src.replace(".hip", ".o"))
         objs.append(obj)
         jobs.append([hipcc, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         list(ex.map(_run, jobs))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB])
     cxx = os.environ.get("CXX", "g++")

@@ -630,7 +630,7 @@ int tdp_gemm_plan(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t def
   if (workspace_elems < 0) return fail(TDP_EINVAL, "negative workspace");
   if (!plan) return fail(TDP_EINVAL, "null pointer");
   const int64_t Npad = epilogue == 2 ? 2 * round_up(N / 2, 128) : round_up(N, 256);
-  const GemmPlan p = gemm_plan({M, 0, 0, epilogue == 2 ? EPI_SWIGLU : epilogue ? EPI_RESIDUAL : EPI_STORE, deferred != 0, Npad, K,
+  const GemmPlan p = gemm_plan({M, 0, 0, epilogue == 2 ? EPI_SWIGLU : epilogue ? EPI_RESIDUAL : EPI_STORE, deferred != 0, false, Npad, K,
                                 workspace_elems});
   plan[0] = p.tile;
   gemm_tile_size(p.tile, plan + 1, plan + 2);
@@ -772,11 +772,20 @@ struct tdp_ends {
   int64_t v_pad = 0;
   uint16_t* table = nullptr;   // bf16 [vocab][d]
   float* gain = nullptr;       // [d]
-  uint16_t* w_head = nullptr;  // bf16, pair-interleaved [v_pad][d]
+  // the vocabulary projection: bf16 [v_pad][d] in layout_weights, or (int8) codes [v_pad][d_pad] with scales
+  uint16_t* w_head = nullptr;
+  bool int8 = false;
+  int64_t d_pad = 0;           // d rounded up to the 128 codes of a k-tile
+  uint8_t* head_codes = nullptr;
+  float* head_scale = nullptr;  // [v_pad]
+  uint8_t* y_codes = nullptr;   // [max_tokens ^ 2][d_pad]: normalised rows as codes
+  float* y_scale = nullptr;     // [max_tokens]
   uint16_t* rows = nullptr;    // bf16 [max_tokens][d]: gathered input rows
   uint16_t* y = nullptr;       // bf16, pair-interleaved [max_tokens ^ 2][d]: normalised rows
   float* logits = nullptr;     // [max_tokens][vocab]
   float* row_max = nullptr;    // the largest logit of every piece of a row
+  float *row_sum = nullptr, *row_weighted = nullptr, *target_logit = nullptr;  // the rest of RowStatistics
+  int device = 0;
   float* ws = nullptr;
   int64_t ws_elems = 0;
 };
@@ -792,6 +801,8 @@ int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out) {
   tdp_ends* e = new (std::nothrow) tdp_ends();
   if (!e) return fail(TDP_ENOMEM, "host allocation failed");
   e->cfg = *cfg;
+  (void)hipGetDevice(&e->device);
+  e->d_pad = round_up(cfg->d_model, 128);
   const int64_t d = cfg->d_model, V = cfg->vocab_size;
   e->v_pad = round_up(V, 256);
   const int64_t M = ((int64_t)cfg->max_tokens + 1) & ~1ll;
@@ -805,7 +816,10 @@ int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out) {
   A(&e->rows, M * d, true);
   A(&e->y, M * d, true);
   A(&e->logits, (int64_t)cfg->max_tokens * V, false);
-  if (V >= kRowMaxColumns) A(&e->row_max, (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth), false);
+  A(&e->row_max, (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth), false);
+  A(&e->row_sum, (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth), false);
+  A(&e->row_weighted, (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth), false);
+  A(&e->target_logit, cfg->max_tokens, false);
   e->ws_elems = 2 * (M < 512 ? M : 512) * e->v_pad;
   A(&e->ws, e->ws_elems, false);
   if (err == hipSuccess) err = hipDeviceSynchronize();
@@ -821,12 +835,31 @@ int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out) {
 void tdp_ends_destroy(tdp_ends* e) {
   if (!e) return;
   (void)hipDeviceSynchronize();
-  void* ptrs[] = {e->table, e->gain, e->w_head, e->rows, e->y, e->logits, e->row_max, e->ws};
+  void* ptrs[] = {e->table, e->gain, e->w_head, e->rows, e->y, e->logits, e->row_max, e->row_sum, e->row_weighted, e->target_logit, e->ws,
+                  e->head_codes, e->head_scale, e->y_codes, e->y_scale};
   for (void* p : ptrs)
     if (p) (void)hipFree(p);
   delete e;
 }
 
+// The memory of the vocabulary projection in the form that is wanted, zeroed: what the form needs and does not have yet.  The other form's is
+// kept: a graph that was captured before still reads it.
+static hipError_t head_memory(tdp_ends* e, bool int8) {
+  const int64_t d = e->cfg.d_model, M = ((int64_t)e->cfg.max_tokens + 1) & ~1ll;
+  hipError_t err = hipSuccess;
+  auto A = [&](auto** p, int64_t n) {
+    if (!*p && err == hipSuccess) err = dev_alloc(p, n, true);
+  };
+  if (!int8) {
+    A(&e->w_head, e->v_pad * d);
+  } else {
+    A(&e->head_codes, e->v_pad * e->d_pad);
+    A(&e->head_scale, e->v_pad);
+    A(&e->y_codes, M * e->d_pad);
+    A(&e->y_scale, e->cfg.max_tokens);
+  }
+  return err;
+}
 int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dtype, int32_t mem, int64_t rows,
                         int64_t cols) {
   if (!e || !src) return fail(TDP_EINVAL, "null ends object or source");
@@ -837,7 +870,7 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   switch (which) {
     case TDP_E_EMBEDDING: er = V; ec = d; break;
     case TDP_E_FINAL_NORM: er = d; ec = 1; break;
-    case TDP_E_LM_HEAD: er = d; ec = V; break;
+    case TDP_E_LM_HEAD: case TDP_E_LM_HEAD_I8: er = d; ec = V; break;
     default: return fail(TDP_EINVAL, "unknown weight id");
   }
   if (rows != er || cols != ec) return fail(TDP_EINVAL, "weight shape does not match the configuration");
@@ -854,12 +887,21 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
     dsrc = tmp;
   }
   const int f32 = dtype == TDP_F32;
-  hipError_t err;
-  if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);
-  else if (which == TDP_E_FINAL_NORM) err = launch_convert_vec(dsrc, f32, d, e->gain, 0);
-  else err = launch_repack(dsrc, f32, d, V, e->w_head, d, 0, 0, 0);
+  const bool head = which == TDP_E_LM_HEAD || which == TDP_E_LM_HEAD_I8, int8 = which == TDP_E_LM_HEAD_I8;
+  hipError_t err = hipSuccess;
+  unsigned* column_max = nullptr;
+  if (head) err = head_memory(e, int8);
+  if (int8 && err == hipSuccess) err = dev_alloc(&column_max, V, false);
+  if (err == hipSuccess) {
+    if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);
+    else if (which == TDP_E_FINAL_NORM) err = launch_convert_vec(dsrc, f32, d, e->gain, 0);
+    else if (!int8) err = launch_repack(dsrc, f32, d, V, e->w_head, d, 0, 0, 0);
+    else err = launch_quantise_weights(dsrc, f32 ? kWeightF32 : kWeightBf16, nullptr, d, V, V, 0, e->head_codes, e->d_pad, e->head_scale, column_max, 0);
+  }
   if (err == hipSuccess) err = hipDeviceSynchronize();
   if (tmp) (void)hipFree(tmp);
+  if (column_max) (void)hipFree(column_max);
+  if (head && err == hipSuccess) e->int8 = int8;
   if (err != hipSuccess) return fail_hip(err, "weight conversion");
   return TDP_OK;
 }
@@ -874,41 +916,120 @@ int tdp_embed_tokens(tdp_ends* e, const int32_t* token_ids, int32_t M, void* hid
   return TDP_OK;
 }
 
-int tdp_lm_head(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int32_t* row_index, int32_t M,
-                float* logits_out, int32_t* next_token, void* stream) {
+// Checks that the calls behind the last stage share; *done: there is nothing to do.
+static int check_head_call(const tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int32_t* row_index, int32_t M, bool* done) {
+  *done = true;
   if (!e) return fail(TDP_EINVAL, "null ends object");
   if (M < 0 || n_rows_in < 0) return fail(TDP_EINVAL, "negative size");
   if (M > e->cfg.max_tokens) return fail(TDP_EINVAL, "M exceeds max_tokens");
   if (M == 0) return TDP_OK;
   if (!hidden_in || n_rows_in < 1) return fail(TDP_EINVAL, "no input rows");
   if (!row_index && M > n_rows_in) return fail(TDP_EINVAL, "M exceeds the input rows");
-  hipStream_t s = (hipStream_t)stream;
+  *done = false;
+  return TDP_OK;
+}
+
+// Final norm and vocabulary projection: logits[m] = RMSNorm(x; gain) * W_head, fp32 [M][V].  The norm hands its rows on in bf16, or as codes to a
+// projection in 8 bits.  What is noted of the logits on the way, if the plan allows it (*width > 0): row_max, or all of `stats`.
+static hipError_t project_rows(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int32_t* row_index, int M, float* logits,
+                               float* row_max, const RowStatistics* stats, int* width, hipStream_t s) {
   const int d = e->cfg.d_model, V = e->cfg.vocab_size;
   const void* x = hidden_in;
+  hipError_t err = hipSuccess;
   if (row_index) {
-    HIP_TRY(launch_gather_rows(hidden_in, d, n_rows_in, row_index, M, d, e->rows, d, s));
+    err = launch_gather_rows(hidden_in, d, n_rows_in, row_index, M, d, e->rows, d, s);
     x = e->rows;
   }
-  HIP_TRY(launch_rmsnorm(x, 0, d, e->gain, e->cfg.rms_eps, M, d, e->y, layout_paired(d), s));
-  float* logits = logits_out ? logits_out : e->logits;
+  if (err == hipSuccess)
+    err = e->int8 ? launch_quantise_rows(x, 0, d, e->gain, e->cfg.rms_eps, M, d, e->d_pad, e->y_codes, e->y_scale, s)
+                  : launch_rmsnorm(x, 0, d, e->gain, e->cfg.rms_eps, M, d, e->y, layout_paired(d), s);
+  if (err != hipSuccess) return err;
   GemmArgs g;
   memset(&g, 0, sizeof(g));
-  g.A = e->y; g.a_layout = layout_paired(d); g.W = e->w_head; g.Kpad = d; g.Npad = e->v_pad; g.M = M; g.N_store = V;
+  if (e->int8) {
+    g.A = e->y_codes; g.a_scale = e->y_scale; g.W = e->head_codes; g.w_scale = e->head_scale; g.Kpad = e->d_pad / 2;
+  } else {
+    g.A = e->y; g.W = e->w_head; g.Kpad = d;
+  }
+  g.a_layout = layout_paired(g.Kpad); g.Npad = e->v_pad; g.M = M; g.N_store = V;
   g.out = logits; g.ldo = V; g.epilogue = EPI_STORE; g.out_f32 = 1;
   g.workspace = e->ws; g.workspace_elems = e->ws_elems;
+  g.row_max = row_max;
+  g.stats = stats;
+  g.row_max_width = width;
+  return launch_gemm(g, s);
+}
+
+int tdp_lm_head(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int32_t* row_index, int32_t M,
+                float* logits_out, int32_t* next_token, void* stream) {
+  bool done;
+  const int rc = check_head_call(e, hidden_in, n_rows_in, row_index, M, &done);
+  if (rc != TDP_OK || done) return rc;
+  hipStream_t s = (hipStream_t)stream;
+  const int V = e->cfg.vocab_size;
+  float* logits = logits_out ? logits_out : e->logits;
   // The greedy token of a long row: the projection notes the largest logit of every piece of it, and a wave looks at those and at
   // one piece, instead of a workgroup at all logits again (final norm to token, 512 rows of 32000 at d 8192: 224 -> 213 us; 300 at
   // 5120: 123 -> 115; 4 rows of a toy width 14.8 -> 12.4).  From 4000 columns on that is never behind by more than the 0.3 us of repeated runs
   // (ten batches of 1 to 512 rows, d 256 to 8192): 512 rows of 4000 / 8004 at d 256 16.6 -> 13.6 / 21.9 -> 15.3, at 5120 35.8 -> 34.6 /
-  // 51.1 -> 48.5.  At 2000 columns the two are level, within 0.5 us either way.
+  // 51.1 -> 48.5.  At 2000 columns the two are level, within 0.5 us either way.  (A projection in 8 bits notes all statistics: it has no
+  // kernels for the maxima alone.)
   int width = 0;
-  g.row_max = next_token && V >= kRowMaxColumns ? e->row_max : nullptr;
-  g.row_max_width = &width;
-  HIP_TRY(launch_gemm(g, s));
+  const bool note = next_token && V >= kRowMaxColumns;
+  const RowStatistics stats{e->row_max, e->row_sum, e->row_weighted, nullptr, nullptr, 1};
+  HIP_TRY(project_rows(e, hidden_in, n_rows_in, row_index, M, logits, note ? e->row_max : nullptr, note && e->int8 ? &stats : nullptr, &width, s));
   if (next_token && width > 0)
     HIP_TRY(launch_argmax_pieces(e->row_max, (int)(e->v_pad / width), width, logits, V, M, V, next_token, s));
   else if (next_token)
     HIP_TRY(launch_argmax_rows(logits, V, M, V, next_token, s));
+  return TDP_OK;
+}
+
+// What both calls for log-probabilities want of their results.
+static int check_logprob_results(int32_t n_top, int32_t n, const int32_t* top_index, const float* top_logprob) {
+  if (n_top < 0 || n_top > TDP_MAX_TOP || n_top > n) return fail(TDP_EINVAL, "n_top must be 0 .. TDP_MAX_TOP and at most the number of columns");
+  if (n_top > 0 && (!top_index || !top_logprob)) return fail(TDP_EINVAL, "n_top > 0 needs top_index and top_logprob");
+  return TDP_OK;
+}
+
+int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int32_t* row_index, int32_t M,
+                         const int32_t* targets, int32_t n_top, int32_t* next_token, float* logprob, float* entropy,
+                         int32_t* top_index, float* top_logprob, void* stream) {
+  bool done;
+  int rc = check_head_call(e, hidden_in, n_rows_in, row_index, M, &done);
+  if (rc == TDP_OK && e) rc = check_logprob_results(n_top, e->cfg.vocab_size, top_index, top_logprob);
+  if (rc != TDP_OK || done) return rc;
+  int dev = -1;
+  HIP_TRY(hipGetDevice(&dev));
+  if (dev != e->device) return fail(TDP_EINVAL, "the object was created on another device than the current one");
+  hipStream_t s = (hipStream_t)stream;
+  const int V = e->cfg.vocab_size;
+  // The projection's epilogue makes the statistics of every piece of a row from the logits in its registers; they are stored only for the
+  // tokens, which are looked for in a few pieces of a row.  (A split projection stores them and they are read again.)
+  const LogprobArgs a{targets, n_top, next_token, logprob, entropy, top_index, top_logprob};
+  const RowStatistics stats{e->row_max, e->row_sum, e->row_weighted, targets, e->target_logit, next_token || n_top > 0};
+  int width = 0;
+  try {
+    HIP_TRY(project_rows(e, hidden_in, n_rows_in, row_index, M, e->logits, nullptr, &stats, &width, s));
+  } catch (...) {  // (the plan is remembered)
+    return fail(TDP_ENOMEM, "host allocation failed");
+  }
+  if (width > 0) HIP_TRY(launch_logprob_pieces(stats, (int)(e->v_pad / width), width, e->logits, V, M, V, a, s));
+  else HIP_TRY(launch_logprob_rows(e->logits, 0, V, M, V, a, s));
+  return TDP_OK;
+}
+
+int tdp_logprob_rows(const void* logits, int32_t dtype, int32_t M, int32_t n, int64_t ld, const int32_t* targets, int32_t n_top,
+                     float* logprob, float* entropy, int32_t* top_index, float* top_logprob, void* stream) {
+  if (dtype != TDP_F32 && dtype != TDP_BF16) return fail(TDP_EINVAL, "dtype must be TDP_F32 or TDP_BF16");
+  if (M < 0 || n < 1 || n > (1 << 30) || ld < n) return fail(TDP_EINVAL, "bad shape");
+  const int rc = check_logprob_results(n_top, n, top_index, top_logprob);
+  if (rc != TDP_OK) return rc;
+  if (M == 0) return TDP_OK;
+  if (!logits) return fail(TDP_EINVAL, "null pointer");
+  if ((uintptr_t)logits & (dtype == TDP_F32 ? 3 : 1)) return fail(TDP_EINVAL, "logits must be aligned to their type");
+  const LogprobArgs a{targets, n_top, nullptr, logprob, entropy, top_index, top_logprob};
+  HIP_TRY(launch_logprob_rows(logits, dtype == TDP_BF16, ld, M, n, a, (hipStream_t)stream));
   return TDP_OK;
 }
 

@@ -1,5 +1,6 @@
 // Device-side helpers shared by the HIP kernels of the stage library (gfx950 only).
 #pragma once
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -11,6 +12,7 @@ typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 
 constexpr int kWave = 64;
 
@@ -148,6 +150,38 @@ __device__ __forceinline__ void take_best_of_lane(Best& b, int lane_xor) {
   const float v = __shfl_xor(b.value, lane_xor, 64);
   const int i = __shfl_xor(b.index, lane_xor, 64);
   take_best(b, v, i);
+}
+
+// What a row of logits z is reduced to for log-probabilities: m = max z, s = sum e^(z - m), t = sum (z - m) e^(z - m).  Then
+// ln p_j = z_j - m - ln s, and the entropy - sum p ln p = ln s - t / s: relative to m, so that nothing cancels.  s and t refer to
+// max(m, -FLT_MAX), which leaves e^(z - m) = 0 where there is nothing but minus infinity; a NaN or plus infinity makes s (and t) NaN.
+struct LogSum {
+  float max, sum, weighted;
+};
+__device__ __forceinline__ LogSum no_logits() { return LogSum{-INFINITY, 0.f, 0.f}; }
+__device__ __forceinline__ float reference_of(float max) { return fmaxf(max, -FLT_MAX); }
+// one more logit, which l.max already counts
+__device__ __forceinline__ void add_logit(LogSum& l, float z) {
+  const float d = z - reference_of(l.max), e = __expf(d);
+  l.sum += e;
+  l.weighted += e * fmaxf(d, -1e30f);  // (where e is 0: 0 times something finite)
+}
+// relative to a larger maximum
+__device__ __forceinline__ void raise(LogSum& l, float max) {
+  const float d = reference_of(l.max) - reference_of(max), e = __expf(d);
+  l.weighted = e * (l.weighted + fmaxf(d, -1e30f) * l.sum);
+  l.sum *= e;
+  l.max = max;
+}
+__device__ __forceinline__ void join(LogSum& l, LogSum o) {
+  const float max = fmaxf(l.max, o.max);
+  raise(l, max);
+  raise(o, max);
+  l.sum += o.sum;
+  l.weighted += o.weighted;
+}
+__device__ __forceinline__ LogSum of_lane(const LogSum& l, int lane_xor) {
+  return LogSum{__shfl_xor(l.max, lane_xor, 64), __shfl_xor(l.sum, lane_xor, 64), __shfl_xor(l.weighted, lane_xor, 64)};
 }
 
 __device__ __forceinline__ float wave_sum(float v) {

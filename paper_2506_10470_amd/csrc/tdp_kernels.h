@@ -43,6 +43,15 @@ struct GemmPlan {
   int tile, splits, chunk;  // chunk: k-tiles of 64 per chunk, 0 = all of K (of a split) in one sum
 };
 struct PrefillRotation;
+// Where a vocabulary projection leaves what log-probabilities are made of: of piece i of row m (width columns, see GemmArgs::stats), at
+// [m * count + i], the largest logit, s = sum e^(z - max) and t = sum (z - max) e^(z - max); where max is minus infinity s = t = 0, with a
+// NaN among them s and t are NaN.  target_logit[m] receives the logit of column targets[m], if there is such a column.
+struct RowStatistics {
+  float *max, *sum, *weighted;
+  const int32_t* targets;  // or null
+  float* target_logit;
+  int store;  // the logits are written to `out` too
+};
 struct GemmArgs {
   const void* A;      // bf16, M rows x Kpad columns in a_layout; rows >= M are never read
   OperandLayout a_layout;
@@ -78,6 +87,13 @@ struct GemmArgs {
   // QKV projection of a prefill, if gemm_can_rotate says that its plan allows it: the epilogue adds the bias, rotates, rounds once, writes
   // queries and values to the bf16 rows and keys to their pages; `out` is not written.
   const PrefillRotation* rotation;  // null = not wanted
+  // The statistics of every row (plain fp32 epilogue without a bias): as row_max, unless the plan splits K; then `out` is written whole
+  // and *row_max_width is 0.
+  const RowStatistics* stats;  // null = not wanted
+  // 8-bit integers: with w_scale (one per weight row, Npad) A and W hold codes, two in the place of a bf16 - Kpad and the layouts count
+  // pairs of codes, Kpad <= 2^16 - and a_scale one per row of A.  out = epilogue(a_scale[m] w_scale[n] sum): EPI_SWIGLU goes to rows of
+  // ldo, in fp32 if out_f32.  No rotation, row_max, splits_used or chunks.
+  const float *a_scale, *w_scale;
 };
 constexpr int kRowMaxWidth = 64;  // the smallest width
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t s);
@@ -87,14 +103,16 @@ bool gemm_can_rotate(const GemmArgs& a);
 struct GemmPlanKey {
   int M, force_tile, force_splits, epilogue;
   bool defer;  // the partials of a split are left to the consumer (GemmArgs::splits_used)
+  bool integers;  // operands of 8-bit integers
   int64_t Npad, Kpad, workspace_elems;
   bool operator==(const GemmPlanKey& o) const {
     return M == o.M && force_tile == o.force_tile && force_splits == o.force_splits && epilogue == o.epilogue &&
-           defer == o.defer && Npad == o.Npad && Kpad == o.Kpad && workspace_elems == o.workspace_elems;
+           defer == o.defer && integers == o.integers && Npad == o.Npad && Kpad == o.Kpad && workspace_elems == o.workspace_elems;
   }
 };
 GemmPlan gemm_plan(const GemmPlanKey& key);
 bool gemm_form_fits(const GemmPlan& form, int M, int64_t Npad, int64_t Kpad, int64_t workspace_elems);
+bool gemm_form_fits_integers(const GemmPlan& form, int M, int64_t Npad, int64_t Kpad, int64_t workspace_elems);  // (GemmArgs::w_scale)
 void gemm_tile_size(int tile, int* rows, int* weight_rows);
 hipError_t gemm_setup();  // one-time function attributes (dynamic LDS size)
 
@@ -118,6 +136,36 @@ hipError_t launch_argmax_rows(const float* logits, int64_t ld, int M, int n, int
 // The same where the largest elements of the pieces [i width, (i + 1) width) are known: row_max[m * count + i]
 hipError_t launch_argmax_pieces(const float* row_max, int count, int width, const float* logits, int64_t ld, int M, int n,
                                 int32_t* out, hipStream_t s);
+
+// Log-probabilities of rows of logits (fp32 or bf16, rows ld elements apart, at any alignment): every pointer of the answer but
+// top_index / top_logprob (with n_top > 0) may be null.
+struct LogprobArgs {
+  const int32_t* targets;  // [M]: the tokens that logprob is of (outside [0, n): minus infinity); null: of the row's largest logit
+  int n_top;               // 0 .. 32, <= n
+  int32_t* next_token;     // as launch_argmax_rows
+  float *logprob, *entropy;
+  int32_t* top_index;      // [M][n_top], -1 behind the last logit that is a number
+  float* top_logprob;
+};
+hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t ld, int M, int n, const LogprobArgs& a, hipStream_t s);
+// The same where the statistics of pieces of `width` columns are known (count to a row), the targets' logits among them; logits (16-byte
+// aligned, n and ld multiples of 4) are read for tokens only.
+hipError_t launch_logprob_pieces(const RowStatistics& st, int count, int width, const float* logits, int64_t ld, int M, int n,
+                                 const LogprobArgs& a, hipStream_t s);
+
+// ---- 8-bit integers ---------------------------------------------------------------------------
+// A vector v is held as codes c and a scale: with a = max |v|, scale = a / 127 and c = rint(v * (127 / a)), every operation rounded in
+// fp32.  Zeros: scale 0.  A vector with an infinity or a NaN: scale NaN, codes 0.  (Below 2^-100, v and a are multiplied by 2^100 for the
+// codes: 127 / a would overflow.)
+// Rows of x (bf16 or fp32, K a multiple of 8, 16-byte aligned) -> codes in layout_paired(Kpad / 2), zeros from K to Kpad (a multiple of
+// 128), and scales [M].  With a gain the row is RMSNorm(x; gain): codes of x * gain, the scale times 1 / sqrt(mean x^2 + eps).
+hipError_t launch_quantise_rows(const void* x, int x_is_f32, int64_t ldx, const float* gain, float eps, int M, int K, int64_t Kpad,
+                                void* codes, float* scales, hipStream_t s);
+// Columns of src [K][ld] (N of them) -> rows of codes in layout_weights(Kpad / 2) and scales, weight row row_of(n) as launch_repack's mode.
+// From codes: copied, with their scales.  column_max: scratch [N].
+enum WeightKind : int { kWeightBf16 = 0, kWeightF32 = 1, kWeightCodes = 2 };
+hipError_t launch_quantise_weights(const void* src, int kind, const float* src_scales, int64_t K, int64_t N, int64_t ld, int mode,
+                                   void* dst, int64_t Kpad, float* scales, unsigned* column_max, hipStream_t s);
 
 // ---- RMSNorm ---------------------------------------------------------------------------------
 hipError_t launch_rmsnorm(const void* x, int x_is_f32, int64_t ldx, const float* gain, float eps, int M, int d,

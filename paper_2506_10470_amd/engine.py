@@ -10,7 +10,7 @@ kernels, on the stream the caller names.  Host logic only: no arithmetic of the 
 """
 from __future__ import annotations
 
-from typing import Dict, List, Sequence, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -32,8 +32,10 @@ class StageWorker:
 
     def __init__(self, tdp, stage: int, ends: int, d_model: int, num_pages: int, max_pages_per_seq: int,
                  max_batch: int, max_tokens: int, max_seqs: int, prompts: Sequence[Sequence[int]], stream=None,
-                 check_tables: bool = False):
-        """check_tables: validate every call's block tables on the GPU first (tdp_stage_check_*): one
+                 check_tables: bool = False, logprobs: Optional[int] = None):
+        """logprobs: the log-probability of every generated token goes to self.logprobs[i] (beside
+        self.generated[i]), and of the `logprobs` likeliest tokens in its place (0: none) as (token, log-probability) pairs to
+        self.top[i].  check_tables: validate every call's block tables on the GPU first (tdp_stage_check_*): one
         synchronisation per call, for runs that test the allocator rather than the throughput."""
         self.tdp, self.ends = tdp, ends
         self.stages = [stage] if isinstance(stage, int) else list(stage)
@@ -50,7 +52,17 @@ class StageWorker:
         rows = max(max_batch, max_tokens, 1)
         self.hidden = torch.empty((rows, d_model), dtype=torch.bfloat16, device="cuda")
         self.hidden_out = torch.empty_like(self.hidden)
-        self.next_tok = torch.empty(max(max_batch, max_seqs, 1), dtype=torch.int32, device="cuda")
+        answers = max(max_batch, max_seqs, 1)
+        self.next_tok = torch.empty(answers, dtype=torch.int32, device="cuda")
+        if logprobs is not None and not 0 <= logprobs <= tdp.MAX_TOP:
+            raise ValueError("logprobs must be 0 .. %d" % tdp.MAX_TOP)
+        self.n_top = logprobs
+        self.logprobs: List[List[float]] = [[] for _ in prompts]
+        self.top: List[List[List[Tuple[int, float]]]] = [[] for _ in prompts]
+        if logprobs is not None:
+            self.tok_logprob = torch.empty(answers, dtype=torch.float32, device="cuda")
+            self.top_index = torch.empty((answers, logprobs), dtype=torch.int32, device="cuda")
+            self.top_logprob = torch.empty((answers, logprobs), dtype=torch.float32, device="cuda")
         self.stats = {"prefill_batches": 0, "prefill_tokens": 0, "decode_steps": 0, "decode_tokens": 0,
                       "released": 0, "evicted": 0, "min_free_pages": num_pages}
 
@@ -72,6 +84,26 @@ class StageWorker:
     @staticmethod
     def _i32(a) -> torch.Tensor:
         return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+    # ---- behind the last stage
+    def _answer(self, ids: Sequence[int], hidden: torch.Tensor, row_index) -> None:
+        """The next token of every request of a batch, from its row of the last hidden states."""
+        tdp, n = self.tdp, len(ids)
+        if self.n_top is None:
+            tdp.tdp_lm_head(self.ends, hidden, hidden.shape[0], row_index, n, None, self.next_tok[:n], self.stream)
+        else:
+            some = self.n_top > 0
+            tdp.tdp_lm_head_logprobs(self.ends, hidden, hidden.shape[0], row_index, n, None, self.n_top, self.next_tok[:n],
+                                     self.tok_logprob[:n], None, self.top_index if some else None, self.top_logprob if some else None,
+                                     self.stream)
+        tokens = self.next_tok[:n].cpu().tolist()
+        for rid, t in zip(ids, tokens):
+            self.generated[rid].append(int(t))
+        if self.n_top is not None:
+            index, values = self.top_index[:n].cpu().tolist(), self.top_logprob[:n].cpu().tolist()
+            for rid, lp, i, v in zip(ids, self.tok_logprob[:n].cpu().tolist(), index, values):
+                self.logprobs[rid].append(lp)
+                self.top[rid].append(list(zip(i, v)))
 
     # ---- the three events
     def prefill(self, ids: List[int], lens: List[int]) -> None:
@@ -101,9 +133,7 @@ class StageWorker:
             tdp.tdp_stage_prefill(st, x, cu_dev, table, n, total, y, self.stream)
             x, y = y, x
         y = x
-        tdp.tdp_lm_head(self.ends, y, total, self._i32(cu[1:] - 1), n, None, self.next_tok[:n], self.stream)
-        for rid, t in zip(ids, self.next_tok[:n].cpu().tolist()):
-            self.generated[rid].append(int(t))
+        self._answer(ids, y, self._i32(cu[1:] - 1))
         self.stats["prefill_batches"] += 1
         self.stats["prefill_tokens"] += total
 
@@ -131,9 +161,7 @@ class StageWorker:
             tdp.tdp_stage_decode(st, x, ctx_dev, table, n, y, self.stream)
             x, y = y, x
         y = x
-        tdp.tdp_lm_head(self.ends, y, n, None, n, None, self.next_tok[:n], self.stream)
-        for rid, t in zip(ids, self.next_tok[:n].cpu().tolist()):
-            self.generated[rid].append(int(t))
+        self._answer(ids, y, None)
         self.stats["decode_steps"] += 1
         self.stats["decode_tokens"] += n
 

@@ -37,7 +37,12 @@ class EndsConfig(C.Structure):
                 ("max_tokens", C.c_int32)]
 
 
-E_EMBEDDING, E_FINAL_NORM, E_LM_HEAD = 0, 1, 2
+class LinearI8Config(C.Structure):
+    _fields_ = [("in_features", C.c_int32), ("out_features", C.c_int32), ("gated", C.c_int32), ("max_rows", C.c_int32)]
+
+
+E_EMBEDDING, E_FINAL_NORM, E_LM_HEAD, E_LM_HEAD_I8 = 0, 1, 2, 3
+MAX_TOP = 32
 
 
 class TdpError(RuntimeError):
@@ -87,6 +92,15 @@ _SIGS = {
     "tdp_embed_tokens": (C.c_int, [_vp, _vp, _i32, _vp, _vp]),
     "tdp_lm_head": (C.c_int, [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp]),
     "tdp_argmax_rows": (C.c_int, [_vp, _i32, _i32, _i64, _vp, _vp]),
+    "tdp_logprob_rows": (C.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "tdp_lm_head_logprobs": (C.c_int, [_vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "tdp_linear_i8_create": (C.c_int, [C.POINTER(LinearI8Config), C.POINTER(_vp)]),
+    "tdp_linear_i8_destroy": (None, [_vp]),
+    "tdp_linear_i8_set_weight": (C.c_int, [_vp, _vp, _i32, _i32, _i64, _i64]),
+    "tdp_linear_i8_set_codes": (C.c_int, [_vp, _vp, _vp, _i32, _i64, _i64]),
+    "tdp_linear_i8_set_bias": (C.c_int, [_vp, _vp, _i32, _i32, _i64]),
+    "tdp_linear_i8_set_form": (C.c_int, [_vp, _i32, _i32]),
+    "tdp_linear_i8_run": (C.c_int, [_vp, _vp, _i32, _i64, _i32, _vp, _i64, _vp, _i32, _i64, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(lib, _name)
@@ -268,3 +282,45 @@ def tdp_lm_head(e, hidden_in, n_rows_in, row_index, M, logits_out, next_token, s
 
 def tdp_argmax_rows(logits, M, n, ld, out, stream=None) -> None:
     _check(lib.tdp_argmax_rows(_ptr(logits), M, n, ld, _ptr(out), _stream(stream)))
+
+
+def tdp_logprob_rows(logits, dtype, M, n, ld, targets, n_top, logprob, entropy, top_index, top_logprob, stream=None) -> None:
+    _check(lib.tdp_logprob_rows(_ptr(logits), dtype, M, n, ld, _ptr(targets), n_top, _ptr(logprob), _ptr(entropy), _ptr(top_index),
+                                _ptr(top_logprob), _stream(stream)))
+
+
+def tdp_lm_head_logprobs(e, hidden_in, n_rows_in, row_index, M, targets, n_top, next_token, logprob, entropy, top_index, top_logprob,
+                         stream=None) -> None:
+    _check(lib.tdp_lm_head_logprobs(e, _ptr(hidden_in), n_rows_in, _ptr(row_index), M, _ptr(targets), n_top, _ptr(next_token),
+                                    _ptr(logprob), _ptr(entropy), _ptr(top_index), _ptr(top_logprob), _stream(stream)))
+
+
+def tdp_linear_i8_create(cfg: LinearI8Config) -> int:
+    h = _vp()
+    _check(lib.tdp_linear_i8_create(C.byref(cfg), C.byref(h)))
+    return h.value
+
+
+def tdp_linear_i8_destroy(h) -> None:
+    lib.tdp_linear_i8_destroy(h)
+
+
+def tdp_linear_i8_set_weight(h, src, dtype, mem, rows, cols) -> None:
+    _check(lib.tdp_linear_i8_set_weight(h, _ptr(src), dtype, mem, rows, cols))
+
+
+def tdp_linear_i8_set_codes(h, codes, scales, mem, rows, cols) -> None:
+    _check(lib.tdp_linear_i8_set_codes(h, _ptr(codes), _ptr(scales), mem, rows, cols))
+
+
+def tdp_linear_i8_set_bias(h, src, dtype, mem, n) -> None:
+    _check(lib.tdp_linear_i8_set_bias(h, _ptr(src), dtype, mem, n))
+
+
+def tdp_linear_i8_set_form(h, tile: int, splits: int = 1) -> None:
+    _check(lib.tdp_linear_i8_set_form(h, tile, splits))
+
+
+def tdp_linear_i8_run(h, x, x_dtype, ld_x, M, residual, ld_residual, out, out_dtype, ld_out, stream=None) -> None:
+    _check(lib.tdp_linear_i8_run(h, _ptr(x), x_dtype, ld_x, M, _ptr(residual), ld_residual, _ptr(out), out_dtype, ld_out,
+                                 _stream(stream)))

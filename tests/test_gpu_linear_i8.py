@@ -1,0 +1,252 @@
+"""Products in 8-bit integers (tdp_linear_i8_*) against oracle/int8_oracle.py.
+
+Codes and scales are a rule in fp32 that the oracle follows to the bit, and the sums are whole numbers: what is left are roundings.
+With u = 2^-24: a sum's conversion and two products are off by 3 u of the value, a bias and a residual by u of what they give each; a result
+in bf16 by half a step, 2^-8 of its value.  Gated: silu(g) u, with g and u off by 3 u of themselves; the exponent of e^-g is off
+by 4 |g| u and the exponential, the sum, the reciprocal and two products by 8 u: (4 |g| + 16) u of the result in all."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import int8_oracle as Q
+from paper_2506_10470_amd import tdp
+from stage_helpers import f64
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+KIND = {torch.float32: tdp.F32, torch.bfloat16: tdp.BF16}
+
+
+class Linear:
+    def __init__(self, K, N, max_rows, gated=False):
+        self.K, self.N, self.gated, self.cols = K, N, gated, N // 2 if gated else N
+        self.h = tdp.tdp_linear_i8_create(tdp.LinearI8Config(K, N, int(gated), max_rows))
+
+    def codes(self, seed, low=-127):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.w = torch.randint(low, 128, (self.K, self.N), generator=g, device="cuda", dtype=torch.int8)
+        self.s = torch.rand(self.N, generator=g, device="cuda") * 0.01 + 1e-4
+        tdp.tdp_linear_i8_set_codes(self.h, self.w, self.s, tdp.DEVICE, self.K, self.N)
+        return self
+
+    def run(self, x, out_dtype=torch.bfloat16, residual=None, stream=None):
+        out = torch.full((x.shape[0], self.cols), float("nan"), dtype=out_dtype, device="cuda")
+        tdp.tdp_linear_i8_run(self.h, x, KIND[x.dtype], self.K, x.shape[0], residual, self.cols, out, KIND[out_dtype], self.cols, stream)
+        return out
+
+    def exact(self, x):
+        xc, xs = Q.quantise(x.float().cpu().numpy())
+        return Q.product(xc, xs, self.w.cpu().numpy().T, self.s.cpu().numpy())
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        tdp.tdp_linear_i8_destroy(self.h)
+
+
+def rows(M, K, seed, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(M, K, generator=g, device="cuda") * torch.exp(torch.randn(M, 1, generator=g, device="cuda"))).to(dtype)
+
+
+def check(out, y, bias=None, residual=None):
+    ref, slack = y.copy(), 3 * U * np.abs(y)
+    for t in (bias, residual):
+        if t is not None:
+            ref = ref + f64(t)
+            slack = slack + U * np.abs(ref)
+    near(out, ref, slack)
+
+
+def near(out, ref, slack):
+    got = f64(out)
+    if out.dtype == torch.bfloat16:
+        slack = slack + 2.0 ** -8 * (np.abs(ref) + slack)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    fine = ~np.isnan(ref)
+    off = np.abs(got - ref)[fine] - slack[fine]
+    assert (off <= 0).all(), (off.max(), np.argwhere(fine)[off.argmax()])
+
+
+def silu_gate(y):
+    g, u = y[:, :y.shape[1] // 2], y[:, y.shape[1] // 2:]
+    ref = g / (1 + np.exp(-np.clip(g, -700, None))) * u
+    return ref, (4 * np.abs(g) + 16) * U * np.abs(ref) + 1e-30 * np.abs(u)
+
+
+SIZES = [(1, 8, 4), (1, 256, 256), (2, 24, 8), (3, 128, 260), (5, 136, 100), (16, 4096, 512), (31, 1000, 2044), (33, 64, 36), (64, 5120, 1024),
+         (130, 1000, 1000), (200, 520, 516), (257, 128, 4), (300, 264, 2048), (513, 8, 1028), (1100, 2048, 260)]
+
+
+@pytest.mark.parametrize("x_dtype,out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32), (torch.bfloat16, torch.float32),
+                                               (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_plain_bias_and_residual(M, K, N, x_dtype, out_dtype):
+    with Linear(K, N, M).codes(M + K + N, low=-128) as lin:
+        x = rows(M, K, K + N, x_dtype)
+        y = lin.exact(x)
+        check(lin.run(x, out_dtype), y)
+        residual = rows(M, N, 5, out_dtype)
+        check(lin.run(x, out_dtype, residual), y, None, residual)
+        bias = torch.randn(N, device="cuda")
+        tdp.tdp_linear_i8_set_bias(lin.h, bias, tdp.F32, tdp.DEVICE, N)
+        check(lin.run(x, out_dtype), y, bias)
+        check(lin.run(x, out_dtype, residual), y, bias, residual)
+        in_place = residual.clone()
+        tdp.tdp_linear_i8_run(lin.h, x, KIND[x_dtype], K, M, in_place, N, in_place, KIND[out_dtype], N)
+        assert torch.equal(in_place, lin.run(x, out_dtype, residual))
+
+
+@pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,K,F", [(1, 256, 688), (3, 8, 4), (17, 4096, 36), (48, 1000, 132), (200, 512, 1376), (520, 136, 260)])
+def test_gated(M, K, F, out_dtype):
+    with Linear(K, 2 * F, M, True).codes(M + F) as lin:
+        x = rows(M, K, 3)
+        ref, slack = silu_gate(lin.exact(x))
+        near(lin.run(x, out_dtype), ref, slack)
+
+
+TILES = [1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 12, 13]
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_every_tile_gives_the_same_bits(tile):
+    """Whole and partly filled tiles, K over several turns of every ring, uneven splits; every epilogue, both result types."""
+    for M, K, N in ((300, 2184, 1028), (40, 4096, 516)):
+        with Linear(K, N, 512).codes(1) as plain, Linear(K, 2 * N, 512, True).codes(2) as gated:
+            x, residual = rows(M, K, 9), rows(M, N, 10)
+            bias = torch.randn(N, device="cuda")
+            want = [plain.run(x), plain.run(x, residual=residual), gated.run(x), gated.run(x, torch.float32)]
+            check(want[0], plain.exact(x))
+            tdp.tdp_linear_i8_set_bias(plain.h, bias, tdp.F32, tdp.DEVICE, N)
+            want += [plain.run(x, torch.float32), plain.run(x, residual=residual)]
+            zero = torch.zeros(N, device="cuda")
+            for splits in (1, 2, 5, 6):
+                tdp.tdp_linear_i8_set_bias(plain.h, zero, tdp.F32, tdp.DEVICE, N)
+                for lin in (plain, gated):
+                    tdp.tdp_linear_i8_set_form(lin.h, tile, splits)
+                got = [plain.run(x), plain.run(x, residual=residual), gated.run(x), gated.run(x, torch.float32)]
+                tdp.tdp_linear_i8_set_bias(plain.h, bias, tdp.F32, tdp.DEVICE, N)
+                got += [plain.run(x, torch.float32), plain.run(x, residual=residual)]
+                for a, b in zip(want, got):
+                    assert torch.equal(a, b), (M, splits)
+
+
+def test_a_rows_result_does_not_depend_on_the_batch():
+    with Linear(5120, 1024, 600).codes(4) as lin:
+        x = rows(600, 5120, 1)
+        whole = lin.run(x)
+        for M in (1, 2, 17, 64, 129, 257, 512):
+            assert torch.equal(lin.run(x[:M].contiguous()), whole[:M])
+
+
+def test_rows_apart_leave_what_is_between_them():
+    M, K, N = 37, 264, 100
+    with Linear(K, N, 64).codes(4) as lin:
+        wide = torch.full((M, K + 24), float("nan"), dtype=torch.bfloat16, device="cuda")
+        wide[:, :K] = rows(M, K, 2)
+        out = torch.full((M + 3, N + 12), 7.0, dtype=torch.bfloat16, device="cuda")
+        residual = rows(M, N + 4, 6)
+        tdp.tdp_linear_i8_run(lin.h, wide, tdp.BF16, K + 24, M, residual, N + 4, out, tdp.BF16, N + 12)
+        x = wide[:, :K].contiguous()
+        check(out[:M, :N], lin.exact(x), None, residual[:, :N])
+        assert (out[:, N:] == 7).all() and (out[M:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("mem", [tdp.DEVICE, tdp.HOST])
+@pytest.mark.parametrize("gated", [False, True])
+def test_weights_are_quantised_column_by_column(dtype, mem, gated):
+    K, N, M = 520, 136, 12
+    w = (torch.randn(K, N) * 0.02 * torch.exp(torch.randn(N))).to(dtype)
+    w[:, 3] = 0
+    w[5, 9] = float("nan")
+    w[5, 11] = float("inf")
+    w[:, 13] *= 1e-36
+    codes, scales = Q.quantise(w.float().numpy().T)
+    with Linear(K, N, M, gated) as lin:
+        src = (w.cuda() if mem == tdp.DEVICE else w if dtype == torch.float32 else w.view(torch.int16).numpy())
+        tdp.tdp_linear_i8_set_weight(lin.h, src, KIND[dtype], mem, K, N)
+        x = rows(M, K, 1)
+        xc, xs = Q.quantise(x.float().cpu().numpy())
+        y = Q.product(xc, xs, codes, scales)
+        out = lin.run(x, torch.float32)
+        if gated:
+            ref, slack = silu_gate(y)
+            near(out, ref, slack + 1e-37)
+        else:
+            near(out, y, 3 * U * np.abs(y) + 1e-44)     # (results below 2^-126 are multiples of 2^-149)
+            assert np.isnan(f64(out)[:, [9, 11]]).all() and (out[:, 3] == 0).all()
+
+
+def test_codes_and_scales_from_the_host():
+    K, N = 40, 12
+    codes = np.random.default_rng(1).integers(-128, 128, (K, N)).astype(np.int8)
+    scales = np.linspace(0.5, 2, N).astype(np.float32)
+    with Linear(K, N, 4) as lin:
+        tdp.tdp_linear_i8_set_codes(lin.h, codes, scales, tdp.HOST, K, N)
+        x = rows(4, K, 1)
+        xc, xs = Q.quantise(x.float().cpu().numpy())
+        check(lin.run(x, torch.float32), Q.product(xc, xs, codes.T, scales))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_of_zeros_of_small_and_of_no_numbers(dtype):
+    K, N = 264, 64
+    with Linear(K, N, 16).codes(8) as lin:
+        x = rows(8, K, 1, dtype)
+        x[0] = 0
+        x[1] *= 1e-37
+        x[2, 5] = float("nan")
+        x[3, 9] = -float("inf")
+        x[4] *= 1e30
+        x[5] = 0
+        x[5, K - 1] = 3.0
+        y = lin.exact(x)
+        out = lin.run(x, torch.float32)
+        near(out, y, 3 * U * np.abs(y) + 1e-44)
+        assert (out[0] == 0).all() and torch.isnan(out[2:4]).all()
+
+
+def test_the_largest_sums_do_not_overflow():
+    K, N = 131072, 4
+    with Linear(K, N, 2) as lin:
+        w = torch.full((K, N), -128, dtype=torch.int8, device="cuda")
+        w[:, 1] = 127
+        tdp.tdp_linear_i8_set_codes(lin.h, w, torch.ones(N, device="cuda"), tdp.DEVICE, K, N)
+        x = torch.ones((2, K), dtype=torch.bfloat16, device="cuda")
+        x[1] = -1
+        got = f64(lin.run(x, torch.float32))
+        scale = float(np.float32(1) / np.float32(127))
+        for m, sign in ((0, 1), (1, -1)):
+            for n in range(N):
+                want = sign * 127.0 * K * (127 if n == 1 else -128) * scale
+                assert abs(got[m, n] - want) <= 3 * U * abs(want)
+
+
+def test_captured_and_replayed_on_another_stream():
+    M, K, N = 24, 2048, 512
+    with Linear(K, N, M).codes(3) as lin:
+        x, out = rows(M, K, 1), torch.zeros((M, N), dtype=torch.bfloat16, device="cuda")
+        residual = rows(M, N, 2)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            tdp.tdp_linear_i8_run(lin.h, x, tdp.BF16, K, M, residual, N, out, tdp.BF16, N, torch.cuda.current_stream())
+        for seed in range(3):
+            x.copy_(rows(M, K, 20 + seed))
+            graph.replay()
+            torch.cuda.synchronize()
+            want = lin.run(x, residual=residual)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+
+
+def test_calls_back_to_back_on_one_stream_share_the_scratch_in_order():
+    with Linear(1000, 516, 300).codes(3) as lin:
+        xs = [rows(M, 1000, M) for M in (300, 1, 77, 300, 5)]
+        torch.cuda.synchronize()
+        outs = [lin.run(x) for x in xs]
+        for x, out in zip(xs, outs):
+            check(out, lin.exact(x))
