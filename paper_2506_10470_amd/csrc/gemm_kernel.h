@@ -423,11 +423,10 @@ __device__ __forceinline__ void gemm_epilogue16_int(const GemmIntParams& p, f32x
   }
 }
 
-// The statistics of every row among the wave's 16 WT columns, for log-probabilities: with z the logits there and m the largest of them,
-// m, s = sum e^(z - m) and t = sum (z - m) e^(z - m), and the logit of the row's given token where it is among them.  A lane
-// makes them of its own 4 WT logits in registers, relative to its own largest; the four lanes of a row are joined behind all rows'
-// arithmetic, with the exchanges of all row blocks in flight.  Minus infinity adds nothing (0 e^..), a NaN makes s and t NaN.
-// Logits are stored if the call needs them later.
+// The statistics of every row among the wave's 16 WT columns, for log-probabilities (LogSum), and the logit of the row's given token
+// where it is among them.  A lane makes them of its own 4 WT logits in registers, relative to its own largest; the four lanes of
+// a row are joined behind all rows' arithmetic, with the exchanges of all row blocks in flight.  Logits are stored if the call
+// needs them later.
 template <int AT, int WT, typename Params>
 __device__ __forceinline__ void gemm_epilogue16_stats(const Params& p, f32x4 (&acc)[WT][AT], int row0, int col0,
                                                       int l16, int kq) {
@@ -466,10 +465,12 @@ __device__ __forceinline__ void gemm_epilogue16_stats(const Params& p, f32x4 (&a
 #pragma unroll
     for (int wt = 0; wt < WT; ++wt) mx = fmaxf(fmaxf(mx, fmaxf(z[wt][0], z[wt][1])), fmaxf(z[wt][2], z[wt][3]));
     sum[at] = LogSum{mx, 0.f, 0.f};
+    float flat[4 * WT];
 #pragma unroll
     for (int wt = 0; wt < WT; ++wt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) add_logit(sum[at], z[wt][e]);
+      for (int e = 0; e < 4; ++e) flat[4 * wt + e] = z[wt][e];
+    add_logits(sum[at], flat);
     __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll

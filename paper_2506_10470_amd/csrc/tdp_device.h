@@ -152,24 +152,46 @@ __device__ __forceinline__ void take_best_of_lane(Best& b, int lane_xor) {
   take_best(b, v, i);
 }
 
-// What a row of logits z is reduced to for log-probabilities: m = max z, s = sum e^(z - m), t = sum (z - m) e^(z - m).  Then
-// ln p_j = z_j - m - ln s, and the entropy - sum p ln p = ln s - t / s: relative to m, so that nothing cancels.  s and t refer to
-// max(m, -FLT_MAX), which leaves e^(z - m) = 0 where there is nothing but minus infinity; a NaN or plus infinity makes s (and t) NaN.
+// What logits z are reduced to for log-probabilities: the largest, and s = sum 2^x, t = sum x 2^x with x = z log2(e) - r, where the
+// reference r is the largest times log2(e), rounded.  Then, with log2(e) as fp32 holds it,
+//   ln p_j = ln 2 (z_j log2(e) - r - log2 s),      entropy = - sum p ln p = ln 2 (log2 s - t / s):
+// r is a number like any other, so its rounding costs nothing, x is one fused multiply-add, and everything is relative to the
+// largest: nothing large cancels.  (fp32's log2(e) is off by 2^-26 of itself, the same for all logits: as much in the results.)
+// Where z log2(e) leaves fp32 (beyond 2e38) r is the largest itself, -FLT_MAX for minus infinity, and x = (z - r) log2(e).
+// Minus infinity adds nothing.  A NaN or plus infinity makes s and t NaN.
 struct LogSum {
   float max, sum, weighted;
 };
+constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
 __device__ __forceinline__ LogSum no_logits() { return LogSum{-INFINITY, 0.f, 0.f}; }
-__device__ __forceinline__ float reference_of(float max) { return fmaxf(max, -FLT_MAX); }
-// one more logit, which l.max already counts
-__device__ __forceinline__ void add_logit(LogSum& l, float z) {
-  const float d = z - reference_of(l.max), e = __expf(d);
-  l.sum += e;
-  l.weighted += e * fmaxf(d, -1e30f);  // (where e is 0: 0 times something finite)
+__device__ __forceinline__ bool is_far(float max) { return !(fabsf(max) < 2e38f); }
+__device__ __forceinline__ float exponent_of(float z, float max) {
+  return is_far(max) ? (z - fmaxf(max, -FLT_MAX)) * kLog2E : __builtin_fmaf(z, kLog2E, -(max * kLog2E));
 }
-// relative to a larger maximum
+// x 2^x with 0 for x = minus infinity, added up
+__device__ __forceinline__ void add_power(LogSum& l, float x) {
+  const float e = __builtin_amdgcn_exp2f(x);
+  l.sum += e;
+  l.weighted = __builtin_fmaf(e, fmaxf(x, -1e30f), l.weighted);
+}
+// logits that l.max already counts
+template <int N>
+__device__ __forceinline__ void add_logits(LogSum& l, const float (&z)[N]) {
+  if (is_far(l.max)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) add_power(l, exponent_of(z[i], l.max));
+  } else {
+    const float r = l.max * kLog2E;
+#pragma unroll
+    for (int i = 0; i < N; ++i) add_power(l, __builtin_fmaf(z[i], kLog2E, -r));
+  }
+}
+// relative to a larger maximum (or the same).  (The difference is one of two rounded references: a product fused into it would be another.)
 __device__ __forceinline__ void raise(LogSum& l, float max) {
-  const float d = reference_of(l.max) - reference_of(max), e = __expf(d);
-  l.weighted = e * (l.weighted + fmaxf(d, -1e30f) * l.sum);
+#pragma clang fp contract(off)
+  const float x = is_far(l.max) || is_far(max) ? (fmaxf(l.max, -FLT_MAX) - fmaxf(max, -FLT_MAX)) * kLog2E : l.max * kLog2E - max * kLog2E;
+  const float e = __builtin_amdgcn_exp2f(x);
+  l.weighted = e * __builtin_fmaf(fmaxf(x, -1e30f), l.sum, l.weighted);
   l.sum *= e;
   l.max = max;
 }
@@ -179,6 +201,11 @@ __device__ __forceinline__ void join(LogSum& l, LogSum o) {
   raise(o, max);
   l.sum += o.sum;
   l.weighted += o.weighted;
+}
+// ln p of a logit, log_sum = log2 s
+__device__ __forceinline__ float log_probability(float z, float max, float log_sum) {
+  if (is_far(z) || is_far(max)) return (z - max) - kLn2 * log_sum;
+  return kLn2 * (exponent_of(z, max) - log_sum);
 }
 __device__ __forceinline__ LogSum of_lane(const LogSum& l, int lane_xor) {
   return LogSum{__shfl_xor(l.max, lane_xor, 64), __shfl_xor(l.sum, lane_xor, 64), __shfl_xor(l.weighted, lane_xor, 64)};

@@ -44,8 +44,7 @@ struct GemmPlan {
 };
 struct PrefillRotation;
 // Where a vocabulary projection leaves what log-probabilities are made of: of piece i of row m (width columns, see GemmArgs::stats), at
-// [m * count + i], the largest logit, s = sum e^(z - max) and t = sum (z - max) e^(z - max); where max is minus infinity s = t = 0, with a
-// NaN among them s and t are NaN.  target_logit[m] receives the logit of column targets[m], if there is such a column.
+// [m * count + i], the three numbers of a LogSum.  target_logit[m] receives the logit of column targets[m], if there is such a column.
 struct RowStatistics {
   float *max, *sum, *weighted;
   const int32_t* targets;  // or null
