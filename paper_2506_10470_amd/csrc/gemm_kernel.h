@@ -55,10 +55,6 @@ struct GemmIntStatsParams : GemmIntParams {
   RowStatistics stats;
 };
 
-// silu(z) = z / (1 + e^-z), with the hardware reciprocal (1 ulp) in place of an IEEE division: the
-// gated epilogue evaluates it 128 times per lane and tile, and its result is rounded to bf16 anyway.
-__device__ __forceinline__ float silu_f(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
-
 // Residual add and store of four consecutive output columns (plain / residual epilogues).
 __device__ __forceinline__ void store_row4(const GemmParams& p, int m, int n, float (&v)[4]) {
   if (p.bias) {
@@ -465,12 +461,11 @@ __device__ __forceinline__ void gemm_epilogue16_stats(const Params& p, f32x4 (&a
 #pragma unroll
     for (int wt = 0; wt < WT; ++wt) mx = fmaxf(fmaxf(mx, fmaxf(z[wt][0], z[wt][1])), fmaxf(z[wt][2], z[wt][3]));
     sum[at] = LogSum{mx, 0.f, 0.f};
-    float flat[4 * WT];
+    const float r = reference_of(mx);
 #pragma unroll
     for (int wt = 0; wt < WT; ++wt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) flat[4 * wt + e] = z[wt][e];
-    add_logits(sum[at], flat);
+      for (int e = 0; e < 4; ++e) add_distance(sum[at], z[wt][e] - r);
     __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll

@@ -129,14 +129,238 @@ hipError_t launch_quantise_rows(const void* x, int x_is_f32, int64_t ldx, const 
   const OperandLayout lay = layout_paired(Kpad / 2);
 #define TDP_QUANTISE(F32_IN, NORM) \
   quantise_rows_kernel<F32_IN, NORM><<<M, threads, 0, s>>>(x, ldx, gain, eps, K, (int)(Kpad / 8), (uint8_t*)codes, lay, scales)
-  if (gain) {
-    if (x_is_f32) TDP_QUANTISE(true, true);
-    else TDP_QUANTISE(false, true);
-  } else {
-    if (x_is_f32) TDP_QUANTISE(true, false);
-    else TDP_QUANTISE(false, false);
-  }
+  if (gain) TDP_QUANTISE(false, true);
+  else if (x_is_f32) TDP_QUANTISE(true, false);
+  else TDP_QUANTISE(false, false);
 #undef TDP_QUANTISE
+  return hipGetLastError();
+}
+
+// ---- one row or two --------------------------------------------------------------------------------------------------------------
+// For a row or two a tile of 32 rows, its ring to fill, its partials to sum and two or three launches cost more than the weights are to
+// read.  One launch instead: every workgroup quantises the rows itself into LDS and streams weights through registers, the
+// first of them on their way meanwhile.  A wave takes four weight rows, in 1 KiB loads of four rows x four k-blocks of 64 codes, eight of
+// them at a time, and a lane multiplies its 16 codes with those of every row by v_dot4_i32_i8; the lanes of a weight row are added up
+// at the end.  Where there are too few weight rows for the chip the waves of a workgroup share K (slices).
+// Taken where one round of workgroups holds all weight rows (up to 16384 columns): one row of 256 x 256 3.4 us (tiles 5.8), 4096 x 4096
+// 6.3 (11.1), 5120 x 7168 9.4 (13.4), 28672 x 8192 41 (44: 5.8 TB/s); two rows 4.2, 8.0, 10.7, 42.7.  With more weight rows the
+// tiles' longer runs of memory win: 4096 x 32000 26.0 (24.4), 8192 x 57344 in several turns 93 (72).  With four rows a workgroup's own quantisation costs what is
+// saved (4096 x 4096 12 and 11).
+constexpr int kFewRows = 2, kFewWaves = 8, kFewInFlight = 8, kFewLds = 128 * 1024;
+struct FewRowsParams : FewRowsArgs {
+  int slices, groups, blocks_k;  // waves that share K; groups of four weight rows; k-blocks
+};
+
+template <int MM, bool F32_IN, bool NORM>
+__global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const FewRowsParams p) {
+  constexpr int THREADS = 64 * kFewWaves;
+  extern __shared__ __attribute__((aligned(16))) unsigned char few_smem[];
+  __shared__ unsigned red_max[MM][kFewWaves];
+  __shared__ float red_ss[MM][kFewWaves];
+  __shared__ float x_scale[MM];
+  __shared__ int part[kFewWaves][MM][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int turns = (p.blocks_k + 3) / 4, k_lds = turns * 256;  // of 256 codes
+  const int slice = wave % p.slices, per = (turns + p.slices - 1) / p.slices, t0 = slice * per, t1 = min(t0 + per, turns);
+  const int group = blockIdx.x * (kFewWaves / p.slices) + wave / p.slices;
+  const int rr = (lane >> 2) & 3, kb = lane >> 4, c16 = (lane & 3) * 16;
+  // this lane's weight row (past the last group: the last one's, for nothing)
+  const int last = min(group, p.groups - 1), pair = last * 2 + (rr & 1);
+  const int r = p.gated ? (pair / 32) * 64 + pair % 32 + (rr >> 1) * 32 : last * 4 + rr;
+  const uint8_t* const row_base =
+      (const uint8_t*)p.W + (int64_t)(r >> kWeightGroupShift) * (p.Kpad << kWeightGroupShift) + (r & ((1 << kWeightGroupShift) - 1)) * 64 + c16;
+  i32x4 w[kFewInFlight];
+  auto fetch = [&](int t) {  // (a k-block behind the last: any, its codes are zero)
+    const int block = 4 * t + kb;
+    return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(row_base + ((int64_t)(block < p.blocks_k ? block : 0) << (6 + kWeightGroupShift))));
+  };
+  // the rows' largest magnitudes (and sums of squares), then their codes
+  auto load8 = [&](int m, int c, float (&f)[8]) {
+    if constexpr (F32_IN) {
+      const f32x4* q = reinterpret_cast<const f32x4*>((const float*)p.x + (int64_t)m * p.ldx + c * 8);
+      const f32x4 a = q[0], b = q[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = a[i], f[i + 4] = b[i];
+    } else {
+      const bf16x8 a = ld_bf16x8((const bf16*)p.x + (int64_t)m * p.ldx + c * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = (float)a[i];
+    }
+  };
+  auto gained = [&](int c, float (&f)[8]) {
+    if constexpr (NORM) {
+      const f32x4 g0 = *reinterpret_cast<const f32x4*>(p.gain + c * 8), g1 = *reinterpret_cast<const f32x4*>(p.gain + c * 8 + 4);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= i < 4 ? g0[i] : g1[i - 4];
+    }
+  };
+  const int chunks = p.K / 8;
+  constexpr int KEEP = 2;  // chunks of a row that a thread keeps between maximum and codes (8192 elements of a row in all)
+  float keep[MM][KEEP][8], ss[MM];
+  unsigned largest[MM];
+  auto see = [&](int m, int c, float (&f)[8]) {
+    if constexpr (NORM) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss[m] += f[i] * f[i];
+      gained(c, f);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) largest[m] = max(largest[m], magnitude(f[i]));
+  };
+#pragma unroll
+  for (int m = 0; m < MM; ++m) {
+    largest[m] = 0;
+    ss[m] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+      if (m < p.M && tid + k * THREADS < chunks) load8(m, tid + k * THREADS, keep[m][k]);
+  }
+#pragma unroll
+  for (int m = 0; m < MM; ++m)
+#pragma unroll 2
+    for (int c = tid + KEEP * THREADS; m < p.M && c < chunks; c += THREADS) {
+      float f[8];
+      load8(m, c, f);
+      see(m, c, f);
+    }
+  // (behind the loads of the rows: loads are waited for in order)
+#pragma unroll
+  for (int u = 0; u < kFewInFlight; ++u)
+    if (t0 + u < t1) w[u] = fetch(t0 + u);
+#pragma unroll
+  for (int m = 0; m < MM; ++m)
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k)
+      if (m < p.M && tid + k * THREADS < chunks) see(m, tid + k * THREADS, keep[m][k]);
+#pragma unroll
+  for (int m = 0; m < MM; ++m) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) largest[m] = max(largest[m], (unsigned)__shfl_xor((int)largest[m], o, 64));
+    if constexpr (NORM) ss[m] = wave_sum(ss[m]);
+    if (lane == 0) {
+      red_max[m][wave] = largest[m];
+      red_ss[m][wave] = ss[m];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < MM; ++m) {
+    unsigned all = 0;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kFewWaves; ++i) {
+      all = max(all, red_max[m][i]);
+      sum += red_ss[m][i];
+    }
+    const Quantiser q(all);
+    if (tid == 0) x_scale[m] = NORM ? q.scale * (1.0f / sqrtf(sum / (float)p.K + p.eps)) : q.scale;
+    auto put = [&](int c, const float (&f)[8]) {
+      unsigned o[2] = {0u, 0u};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i / 4] |= (unsigned)(q.code(f[i]) & 255) << (8 * (i % 4));
+      *reinterpret_cast<uint2*>(few_smem + m * k_lds + c * 8) = make_uint2(o[0], o[1]);
+    };
+    if (m < p.M) {
+#pragma unroll
+      for (int k = 0; k < KEEP; ++k)
+        if (tid + k * THREADS < chunks) put(tid + k * THREADS, keep[m][k]);
+#pragma unroll 2
+      for (int c = tid + KEEP * THREADS; c < chunks; c += THREADS) {
+        float f[8];
+        load8(m, c, f);
+        gained(c, f);
+        put(c, f);
+      }
+    }
+    for (int c = (m < p.M ? chunks : 0) + tid; c < k_lds / 8; c += THREADS)
+      *reinterpret_cast<uint2*>(few_smem + m * k_lds + c * 8) = make_uint2(0u, 0u);
+  }
+  __syncthreads();
+  int acc[MM];
+#pragma unroll
+  for (int m = 0; m < MM; ++m) acc[m] = 0;
+  const uint8_t* const code = few_smem + kb * 64 + c16;
+#pragma unroll 1
+  for (int t = t0; t < t1; t += kFewInFlight) {
+#pragma unroll
+    for (int u = 0; u < kFewInFlight; ++u) {
+      if (t + u >= t1) break;
+      const i32x4 v = w[u];
+#pragma unroll
+      for (int m = 0; m < MM; ++m) {
+        const i32x4 a = *reinterpret_cast<const i32x4*>(code + m * k_lds + (t + u) * 256);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[m] = __builtin_amdgcn_sdot4(v[i], a[i], acc[m], false);
+      }
+      if (t + u + kFewInFlight < t1) w[u] = fetch(t + u + kFewInFlight);
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MM; ++m)
+    for (int o : {1, 2, 16, 32}) acc[m] += __shfl_xor(acc[m], o, 64);
+  if (p.slices > 1) {
+    if ((lane & 51) == 0)
+#pragma unroll
+      for (int m = 0; m < MM; ++m) part[wave][m][rr] = acc[m];
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < MM; ++m) {
+      acc[m] = 0;
+      for (int i = 0; i < p.slices; ++i) acc[m] += part[wave - slice + i][m][rr];
+    }
+  }
+  // lane (weight row rr, i of 16) writes row i of the result
+  const int m = kb * 4 + (lane & 3);
+  float v = (float)acc[0] * p.w_scale[r] * x_scale[0];
+#pragma unroll
+  for (int i = 1; i < MM; ++i) v = m == i ? (float)acc[i] * p.w_scale[r] * x_scale[i] : v;
+  int col = r;
+  if (p.gated) {
+    const float up = __shfl_xor(v, 8, 64);
+    v = silu_f(v) * up;
+    col = pair;
+  }
+  if (group >= p.groups || slice != 0 || m >= p.M || (p.gated && rr >= 2)) return;
+  if (p.bias) v += p.bias[r];
+  if (p.residual) v += p.out_f32 ? ((const float*)p.residual)[(int64_t)m * p.ldr + col] : (float)((const bf16*)p.residual)[(int64_t)m * p.ldr + col];
+  if (p.out_f32) ((float*)p.out)[(int64_t)m * p.ldo + col] = v;
+  else ((bf16*)p.out)[(int64_t)m * p.ldo + col] = (bf16)v;
+}
+
+// by rows, and fp32 rows, bf16 rows, normed bf16 rows
+#define TDP_FEW(MM) {few_rows_kernel<MM, true, false>, few_rows_kernel<MM, false, false>, few_rows_kernel<MM, false, true>}
+static void (*const kFewKernels[kFewRows][3])(FewRowsParams) = {TDP_FEW(1), TDP_FEW(2)};
+#undef TDP_FEW
+
+hipError_t few_rows_setup() {
+  hipError_t e = hipSuccess;
+  for (const auto& rows : kFewKernels)
+    for (const auto& kernel : rows)
+      if (e == hipSuccess)
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
+  return e;
+}
+
+static int few_rows_lds(int M, int64_t Kpad) { return M * (int)((Kpad + 255) / 256 * 256); }
+static int few_rows_places(int lds) { return lds <= 72 * 1024 ? 512 : 256; }  // workgroups that the chip holds at once
+static int few_rows_groups(int gated, int cols) { return gated ? cols / 2 : cols / 4; }
+bool few_rows_fit(int M, int64_t Kpad, int gated, int cols) {
+  if (M < 1 || M > kFewRows) return false;
+  const int lds = few_rows_lds(M, Kpad);
+  return lds <= kFewLds && few_rows_groups(gated, cols) <= few_rows_places(lds) * kFewWaves;
+}
+
+hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
+  FewRowsParams p;
+  (FewRowsArgs&)p = a;
+  p.blocks_k = (int)(a.Kpad / 64);
+  p.groups = few_rows_groups(a.gated, a.cols);
+  const int turns = (p.blocks_k + 3) / 4, lds = few_rows_lds(a.M, a.Kpad), places = few_rows_places(lds);
+  // slices until the groups fill the chip, as long as a wave has a few loads
+  p.slices = 1;
+  while (p.slices < kFewWaves && p.groups * p.slices * 2 <= places * kFewWaves && turns >= 4 * p.slices) p.slices *= 2;
+  const int blocks = (p.groups * p.slices + kFewWaves - 1) / kFewWaves;
+  kFewKernels[a.M - 1][a.gain ? 2 : a.x_is_f32 ? 0 : 1]<<<blocks, 64 * kFewWaves, lds, s>>>(p);
   return hipGetLastError();
 }
 
@@ -297,6 +521,7 @@ int tdp_linear_i8_create(const tdp_linear_i8_config* cfg, tdp_linear_i8** out) {
   h->ws_elems = 8 * (M < 512 ? M : 512) * h->Npad;
   if (h->ws_elems > (64ll << 20)) h->ws_elems = 64ll << 20;
   hipError_t e = gemm_setup();
+  if (e == hipSuccess) e = few_rows_setup();
   auto alloc = [&](auto** p, int64_t n, bool zero) {
     const size_t bytes = (size_t)n * sizeof(**p);
     if (e == hipSuccess) e = hipMalloc((void**)p, bytes);
@@ -390,7 +615,13 @@ int tdp_linear_i8_run(tdp_linear_i8* h, const void* x, int32_t x_dtype, int64_t 
   int rc = check_device(h);
   if (rc != TDP_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
-  hipError_t e = launch_quantise_rows(x, x_dtype == TDP_F32, ld_x, nullptr, 0.f, M, K, h->Kpad, h->codes, h->x_scale, s);
+  hipError_t e = hipSuccess;
+  if (!h->form.tile && few_rows_fit(M, h->Kpad, h->cfg.gated, cols)) {
+    e = launch_few_rows({x, x_dtype == TDP_F32, ld_x, nullptr, 0.f, M, K, h->Kpad, h->w, h->w_scale, h->has_bias ? h->bias : nullptr,
+                         h->cfg.gated, cols, residual, ld_residual, out, out_dtype == TDP_F32, ld_out}, s);
+    return e == hipSuccess ? TDP_OK : fail_hip(e, "tdp_linear_i8_run");
+  }
+  e = launch_quantise_rows(x, x_dtype == TDP_F32, ld_x, nullptr, 0.f, M, K, h->Kpad, h->codes, h->x_scale, s);
   if (e == hipSuccess) {
     GemmArgs g;
     memset(&g, 0, sizeof(g));

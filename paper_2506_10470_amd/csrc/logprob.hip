@@ -287,10 +287,11 @@ __device__ __forceinline__ void answer_row(const LogprobArgs& a, RowShared& rs, 
   } else if (TOP) {
     __syncthreads();
   }
-  const float log_sum = __builtin_amdgcn_logf(l.sum);  // (log2)
+  const float log_sum = logf(l.sum);
+  auto logprob = [&](float z) { return (z - l.max) - log_sum; };
   if (tid == 0) {
-    if (a.logprob) a.logprob[m] = a.targets && !has_target ? -INFINITY : log_probability(a.targets ? target_logit : l.max, l.max, log_sum);
-    if (a.entropy) a.entropy[m] = kLn2 * (log_sum - l.weighted / l.sum);
+    if (a.logprob) a.logprob[m] = a.targets && !has_target ? -INFINITY : logprob(a.targets ? target_logit : l.max);
+    if (a.entropy) a.entropy[m] = log_sum - l.weighted / l.sum;
   }
   if constexpr (TOP) {
     const int k = max(a.n_top, a.next_token ? 1 : 0);
@@ -298,7 +299,7 @@ __device__ __forceinline__ void answer_row(const LogprobArgs& a, RowShared& rs, 
       if (place == 0 && a.next_token) a.next_token[m] = index;
       if (place < a.n_top) {
         a.top_index[(int64_t)m * a.n_top + place] = index;
-        a.top_logprob[(int64_t)m * a.n_top + place] = log_probability(value, l.max, log_sum);
+        a.top_logprob[(int64_t)m * a.n_top + place] = logprob(value);
       }
     });
     for (int place = found + tid; place < a.n_top; place += blockDim.x) {  // (a row with fewer logits that are numbers)
@@ -341,22 +342,13 @@ __global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restri
 #pragma unroll
       for (int e = 0; e < kPer; ++e) max = fmaxf(max, Row::value(z[u], e));
     if (max > l.max) raise(l, max);
-    // (short rather than fast; and not for minus infinity, of which masked rows are full: any reference will do for it)
-    if (is_far(max) && max != -INFINITY) {
-#pragma unroll 1
-      for (int i = 0; i < kInFlight * kPer; ++i) {
-        const int v = v0 + i / kPer * threads;
-        if (v < row.body) add_power(l, exponent_of(row.at(row.index(v, i % kPer)), max));
-      }
-      return;
-    }
-    const float r = max == -INFINITY ? 0.f : max * kLog2E;
+    const float r = reference_of(max);
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       if (u > 0 && v0 - tid + u * threads >= row.body) break;  // (the same for all threads)
       asm volatile("" : "+v"(z[u]));  // (bf16: converted here again, the values of two passes would not fit)
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) add_power(l, __builtin_fmaf(Row::value(z[u], e), kLog2E, -r));
+      for (int e = 0; e < kPer; ++e) add_distance(l, Row::value(z[u], e) - r);
     }
   };
   const int target = a.targets ? a.targets[m] : -1, edge_at = row.edge(tid);
@@ -375,7 +367,7 @@ __global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restri
   const float own_max = l.max;
   if (edge_at >= 0) {
     LogSum one{edge, 0.f, 0.f};
-    add_power(one, exponent_of(edge, edge));
+    add_distance(one, edge - reference_of(edge));
     join(l, one);
   }
   answer_row<TOP>(
@@ -435,9 +427,8 @@ hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t 
   if (M <= 0) return hipSuccess;
   const int per = logits_are_bf16 ? 8 : 4, vectors = n / per;
   const bool top = a.n_top > 0 || a.next_token;
-  const int most = top ? 2 : kInFlight;  // vectors of a thread, if 1024 are enough for that
-  int threads = 64;
-  while (threads < 1024 && threads * most < vectors) threads *= 2;
+  int threads = 64;  // two vectors to a thread, if 1024 are enough for that (with tokens or without: one order of the sums)
+  while (threads < 1024 && threads * 2 < vectors) threads *= 2;
   const bool keep = vectors <= threads * kInFlight;
   int shift = 0;  // of the elements that a thread has read
   while ((1 << shift) < (vectors + threads - 1) / threads * per) ++shift;

@@ -891,6 +891,7 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   hipError_t err = hipSuccess;
   unsigned* column_max = nullptr;
   if (head) err = head_memory(e, int8);
+  if (int8 && err == hipSuccess) err = few_rows_setup();
   if (int8 && err == hipSuccess) err = dev_alloc(&column_max, V, false);
   if (err == hipSuccess) {
     if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);
@@ -939,6 +940,11 @@ static hipError_t project_rows(tdp_ends* e, const void* hidden_in, int32_t n_row
   if (row_index) {
     err = launch_gather_rows(hidden_in, d, n_rows_in, row_index, M, d, e->rows, d, s);
     x = e->rows;
+  }
+  if (err == hipSuccess && e->int8 && few_rows_fit(M, e->d_pad, 0, V)) {
+    *width = 0;
+    return launch_few_rows({x, 0, d, e->gain, e->cfg.rms_eps, M, d, e->d_pad, e->head_codes, e->head_scale, nullptr, 0, V, nullptr, 0,
+                            logits, 1, V}, s);
   }
   if (err == hipSuccess)
     err = e->int8 ? launch_quantise_rows(x, 0, d, e->gain, e->cfg.rms_eps, M, d, e->d_pad, e->y_codes, e->y_scale, s)

@@ -152,46 +152,28 @@ __device__ __forceinline__ void take_best_of_lane(Best& b, int lane_xor) {
   take_best(b, v, i);
 }
 
-// What logits z are reduced to for log-probabilities: the largest, and s = sum 2^x, t = sum x 2^x with x = z log2(e) - r, where the
-// reference r is the largest times log2(e), rounded.  Then, with log2(e) as fp32 holds it,
-//   ln p_j = ln 2 (z_j log2(e) - r - log2 s),      entropy = - sum p ln p = ln 2 (log2 s - t / s):
-// r is a number like any other, so its rounding costs nothing, x is one fused multiply-add, and everything is relative to the
-// largest: nothing large cancels.  (fp32's log2(e) is off by 2^-26 of itself, the same for all logits: as much in the results.)
-// Where z log2(e) leaves fp32 (beyond 2e38) r is the largest itself, -FLT_MAX for minus infinity, and x = (z - r) log2(e).
-// Minus infinity adds nothing.  A NaN or plus infinity makes s and t NaN.
+// What logits z are reduced to for log-probabilities: the largest, m, and s = sum e^(z - m), t = sum (z - m) e^(z - m).  Then
+//   ln p_j = (z_j - m) - ln s,      entropy = - sum p ln p = ln s - t / s:
+// everything is relative to m, nothing large cancels, and where one token has nearly all its ln p is as exact as s.  (A reference that
+// is m log2(e), rounded, would save a subtraction per logit, one operation of nine; the rounding comes back in the exponential of
+// the largest, 5e-7 of an ln p near zero where this is 5e-8.)
+// For minus infinity m counts as -FLT_MAX, so that it adds nothing.  A NaN or plus infinity makes s and t NaN.
 struct LogSum {
   float max, sum, weighted;
 };
-constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
 __device__ __forceinline__ LogSum no_logits() { return LogSum{-INFINITY, 0.f, 0.f}; }
-__device__ __forceinline__ bool is_far(float max) { return !(fabsf(max) < 2e38f); }
-__device__ __forceinline__ float exponent_of(float z, float max) {
-  return is_far(max) ? (z - fmaxf(max, -FLT_MAX)) * kLog2E : __builtin_fmaf(z, kLog2E, -(max * kLog2E));
-}
-// x 2^x with 0 for x = minus infinity, added up
-__device__ __forceinline__ void add_power(LogSum& l, float x) {
-  const float e = __builtin_amdgcn_exp2f(x);
+__device__ __forceinline__ float reference_of(float max) { return fmaxf(max, -FLT_MAX); }
+__device__ __forceinline__ float exp_fast(float d) { return __builtin_amdgcn_exp2f(d * 1.44269504f); }
+// one more logit, at d from the reference
+__device__ __forceinline__ void add_distance(LogSum& l, float d) {
+  const float e = exp_fast(d);
   l.sum += e;
-  l.weighted = __builtin_fmaf(e, fmaxf(x, -1e30f), l.weighted);
+  l.weighted = __builtin_fmaf(e, fmaxf(d, -1e30f), l.weighted);  // (of minus infinity: 0 times something finite)
 }
-// logits that l.max already counts
-template <int N>
-__device__ __forceinline__ void add_logits(LogSum& l, const float (&z)[N]) {
-  if (is_far(l.max)) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) add_power(l, exponent_of(z[i], l.max));
-  } else {
-    const float r = l.max * kLog2E;
-#pragma unroll
-    for (int i = 0; i < N; ++i) add_power(l, __builtin_fmaf(z[i], kLog2E, -r));
-  }
-}
-// relative to a larger maximum (or the same).  (The difference is one of two rounded references: a product fused into it would be another.)
+// relative to a larger maximum (or the same)
 __device__ __forceinline__ void raise(LogSum& l, float max) {
-#pragma clang fp contract(off)
-  const float x = is_far(l.max) || is_far(max) ? (fmaxf(l.max, -FLT_MAX) - fmaxf(max, -FLT_MAX)) * kLog2E : l.max * kLog2E - max * kLog2E;
-  const float e = __builtin_amdgcn_exp2f(x);
-  l.weighted = e * __builtin_fmaf(fmaxf(x, -1e30f), l.sum, l.weighted);
+  const float d = reference_of(l.max) - reference_of(max), e = exp_fast(d);
+  l.weighted = e * __builtin_fmaf(fmaxf(d, -1e30f), l.sum, l.weighted);
   l.sum *= e;
   l.max = max;
 }
@@ -202,14 +184,13 @@ __device__ __forceinline__ void join(LogSum& l, LogSum o) {
   l.sum += o.sum;
   l.weighted += o.weighted;
 }
-// ln p of a logit, log_sum = log2 s
-__device__ __forceinline__ float log_probability(float z, float max, float log_sum) {
-  if (is_far(z) || is_far(max)) return (z - max) - kLn2 * log_sum;
-  return kLn2 * (exponent_of(z, max) - log_sum);
-}
 __device__ __forceinline__ LogSum of_lane(const LogSum& l, int lane_xor) {
   return LogSum{__shfl_xor(l.max, lane_xor, 64), __shfl_xor(l.sum, lane_xor, 64), __shfl_xor(l.weighted, lane_xor, 64)};
 }
+
+// silu(z) = z / (1 + e^-z), with the hardware reciprocal (1 ulp) in place of an IEEE division: the
+// gated epilogue evaluates it 128 times per lane and tile, and its result is rounded to bf16 anyway.
+__device__ __forceinline__ float silu_f(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll

@@ -157,9 +157,31 @@ hipError_t launch_logprob_pieces(const RowStatistics& st, int count, int width, 
 // fp32.  Zeros: scale 0.  A vector with an infinity or a NaN: scale NaN, codes 0.  (Below 2^-100, v and a are multiplied by 2^100 for the
 // codes: 127 / a would overflow.)
 // Rows of x (bf16 or fp32, K a multiple of 8, 16-byte aligned) -> codes in layout_paired(Kpad / 2), zeros from K to Kpad (a multiple of
-// 128), and scales [M].  With a gain the row is RMSNorm(x; gain): codes of x * gain, the scale times 1 / sqrt(mean x^2 + eps).
+// 128), and scales [M].  With a gain (x bf16) the row is RMSNorm(x; gain): codes of x * gain, the scale times 1 / sqrt(mean x^2 + eps).
 hipError_t launch_quantise_rows(const void* x, int x_is_f32, int64_t ldx, const float* gain, float eps, int M, int K, int64_t Kpad,
                                 void* codes, float* scales, hipStream_t s);
+// The whole product of a row or two, quantised on the way, in one launch where few_rows_fit: as launch_quantise_rows and launch_gemm on integers, to the bit but
+// for the sum of squares of a norm.
+struct FewRowsArgs {
+  const void* x;  // as in launch_quantise_rows
+  int x_is_f32;
+  int64_t ldx;
+  const float* gain;  // null: no norm
+  float eps;
+  int M, K;
+  int64_t Kpad;          // codes of a row
+  const void* W;         // codes in layout_weights(Kpad / 2)
+  const float *w_scale, *bias;  // [Npad], bias null or [Npad]
+  int gated, cols;       // columns of the result
+  const void* residual;  // null, or rows of ldr, of out's type
+  int64_t ldr;
+  void* out;
+  int out_f32;
+  int64_t ldo;
+};
+hipError_t few_rows_setup();  // function attributes (dynamic LDS size), before the first launch
+bool few_rows_fit(int M, int64_t Kpad, int gated, int cols);
+hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s);
 // Columns of src [K][ld] (N of them) -> rows of codes in layout_weights(Kpad / 2) and scales, weight row row_of(n) as launch_repack's mode.
 // From codes: copied, with their scales.  column_max: scratch [N].
 enum WeightKind : int { kWeightBf16 = 0, kWeightF32 = 1, kWeightCodes = 2 };
