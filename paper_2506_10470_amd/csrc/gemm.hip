@@ -323,7 +323,8 @@ void gemm_tile_size(int tile, int* rows, int* weight_rows) {
 }
 
 static GemmPlan plan_of(const GemmArgs& a) {
-  const bool defer = a.splits_used != nullptr && a.epilogue != EPI_SWIGLU;
+  // (a vocabulary projection is planned alike whether its logits are wanted or their statistics: the same bits)
+  const bool defer = a.splits_used != nullptr && a.epilogue != EPI_SWIGLU && !a.stats;
   return a.form.tile ? a.form
                      : gemm_plan({a.M, a.force_tile, a.force_splits, a.epilogue, defer, a.w_scale != nullptr, a.Npad, a.Kpad, a.workspace_elems});
 }

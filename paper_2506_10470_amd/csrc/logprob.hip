@@ -11,12 +11,15 @@ namespace tdp {
 typedef __attribute__((__vector_size__(4 * sizeof(unsigned)))) unsigned u32x4;
 
 // A row of logits, which may begin and end anywhere in a 16-byte vector of memory: its whole vectors, the `body`, and up to seven elements on
-// either side, the edges, which the first threads hold one each.
-template <typename T>
+// either side, the edges, which the first threads hold one each.  PARTS: the fp32 partials of a split projection, whose sums (in the
+// order of the splits) are the logits.
+template <typename T, bool PARTS = false>
 struct LogitRow {
   static constexpr int kPer = 16 / sizeof(T);
   const T* first;
   int n, off, body;  // elements; in front of the body; whole vectors
+  int parts = 1;
+  int64_t stride = 0;  // elements from a part to the next
   __device__ __forceinline__ LogitRow(const T* row, int n_) : first(row), n(n_) {
     const int lead = (int)(((uintptr_t)row & 15) / sizeof(T));
     off = lead ? kPer - lead : 0;
@@ -26,11 +29,23 @@ struct LogitRow {
   __device__ __forceinline__ int index(int v, int e) const { return off + v * kPer + e; }
   template <bool NT>
   __device__ __forceinline__ u32x4 load(int v) const {
-    const u32x4* const p = reinterpret_cast<const u32x4*>(first + off + (int64_t)v * kPer);
-    if constexpr (NT) return __builtin_nontemporal_load(p);
-    else return *p;
+    const T* const p = first + off + (int64_t)v * kPer;
+    if constexpr (PARTS) {
+      f32x4 sum = *reinterpret_cast<const f32x4*>(p);
+      for (int i = 1; i < parts; ++i) sum += *reinterpret_cast<const f32x4*>(p + i * stride);
+      return __builtin_bit_cast(u32x4, sum);
+    } else if constexpr (NT) {
+      return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    } else {
+      return *reinterpret_cast<const u32x4*>(p);
+    }
   }
-  __device__ __forceinline__ float at(int i) const { return (float)first[i]; }
+  __device__ __forceinline__ float at(int i) const {
+    float z = (float)first[i];
+    if constexpr (PARTS)
+      for (int j = 1; j < parts; ++j) z += first[i + j * stride];
+    return z;
+  }
   // the element on an edge that thread tid holds, or -1
   __device__ __forceinline__ int edge(int tid) const {
     const int i = tid < kPer ? tid : off + body * kPer + tid - kPer;
@@ -315,8 +330,9 @@ __device__ __forceinline__ void answer_row(const LogprobArgs& a, RowShared& rs, 
 constexpr int kInFlight = 8;
 // NT: the loads are marked non-temporal, from 240 MiB on, what the memory-side cache cannot hold beside anything else (1 GB of bf16: 180 -> 172 us, 263 MB of
 // fp32: 46 -> 41); below that logits that a projection has just written may still be there.
-template <typename T, bool TOP, bool KEEP, bool NT>
-__global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int n, int shift, const LogprobArgs a) {
+template <typename T, bool TOP, bool KEEP, bool NT, bool PARTS>
+__global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int n, int parts, int64_t stride,
+                                                               int shift, const LogprobArgs a) {
   __shared__ RowShared rs;
   TopShared* ts = nullptr;
   if constexpr (TOP) {
@@ -326,9 +342,13 @@ __global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restri
   extern __shared__ __attribute__((aligned(16))) unsigned char staged_raw[];  // (TOP and KEEP) StagedUnits of every wave
   StagedUnits& staged = reinterpret_cast<StagedUnits*>(staged_raw)[threadIdx.x >> 6];
   const int m = blockIdx.x, tid = threadIdx.x, threads = blockDim.x;
-  typedef LogitRow<T> Row;
+  typedef LogitRow<T, PARTS> Row;
   constexpr int kPer = Row::kPer;
-  const Row row(logits + (int64_t)m * ld, n);
+  Row row(logits + (int64_t)m * ld, n);
+  if constexpr (PARTS) {
+    row.parts = parts;
+    row.stride = stride;
+  }
   LogSum l = no_logits();
   u32x4 z[kInFlight];
   auto fetch = [&](int v0) {
@@ -423,7 +443,8 @@ __global__ __launch_bounds__(256) void logprob_pieces_kernel(const RowStatistics
       });
 }
 
-hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t ld, int M, int n, const LogprobArgs& a, hipStream_t s) {
+hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t ld, int M, int n, int parts, int64_t stride, const LogprobArgs& a,
+                               hipStream_t s) {
   if (M <= 0) return hipSuccess;
   const int per = logits_are_bf16 ? 8 : 4, vectors = n / per;
   const bool top = a.n_top > 0 || a.next_token;
@@ -434,18 +455,20 @@ hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t 
   while ((1 << shift) < (vectors + threads - 1) / threads * per) ++shift;
   const bool nt = !top && (int64_t)M * n * (16 / per) >= (240ll << 20);
   const size_t lds = top && keep ? threads / 64 * sizeof(StagedUnits) : 0;
-#define TDP_ROWS(T, TOP, KEEP, NT) logprob_rows_kernel<T, TOP, KEEP, NT><<<M, threads, lds, s>>>((const T*)logits, ld, n, shift, a)
-#define TDP_ROWS_OF(T)                                   \
-  do {                                                   \
-    if (top && keep) TDP_ROWS(T, true, true, false);     \
-    else if (top) TDP_ROWS(T, true, false, false);       \
-    else if (keep && nt) TDP_ROWS(T, false, true, true); \
-    else if (keep) TDP_ROWS(T, false, true, false);      \
-    else if (nt) TDP_ROWS(T, false, false, true);        \
-    else TDP_ROWS(T, false, false, false);               \
+#define TDP_ROWS(T, TOP, KEEP, NT, PARTS) \
+  logprob_rows_kernel<T, TOP, KEEP, NT, PARTS><<<M, threads, lds, s>>>((const T*)logits, ld, n, parts, stride, shift, a)
+#define TDP_ROWS_OF(T, PARTS)                                     \
+  do {                                                            \
+    if (top && keep) TDP_ROWS(T, true, true, false, PARTS);       \
+    else if (top) TDP_ROWS(T, true, false, false, PARTS);         \
+    else if (keep && nt) TDP_ROWS(T, false, true, !PARTS, PARTS); \
+    else if (keep) TDP_ROWS(T, false, true, false, PARTS);        \
+    else if (nt) TDP_ROWS(T, false, false, !PARTS, PARTS);        \
+    else TDP_ROWS(T, false, false, false, PARTS);                 \
   } while (0)
-  if (logits_are_bf16) TDP_ROWS_OF(bf16);
-  else TDP_ROWS_OF(float);
+  if (parts > 1) TDP_ROWS_OF(float, true);
+  else if (logits_are_bf16) TDP_ROWS_OF(bf16, false);
+  else TDP_ROWS_OF(float, false);
 #undef TDP_ROWS_OF
 #undef TDP_ROWS
   return hipGetLastError();

@@ -86,8 +86,8 @@ struct GemmArgs {
   // QKV projection of a prefill, if gemm_can_rotate says that its plan allows it: the epilogue adds the bias, rotates, rounds once, writes
   // queries and values to the bf16 rows and keys to their pages; `out` is not written.
   const PrefillRotation* rotation;  // null = not wanted
-  // The statistics of every row (plain fp32 epilogue without a bias): as row_max, unless the plan splits K; then `out` is written whole
-  // and *row_max_width is 0.
+  // The statistics of every row (plain fp32 epilogue without a bias): as row_max, unless the plan splits K; then *row_max_width is 0, and
+  // `out` is written whole, or the partials are left (splits_used).
   const RowStatistics* stats;  // null = not wanted
   // 8-bit integers: with w_scale (one per weight row, Npad) A and W hold codes, two in the place of a bf16 - Kpad and the layouts count
   // pairs of codes, Kpad <= 2^16 - and a_scale one per row of A.  out = epilogue(a_scale[m] w_scale[n] sum): EPI_SWIGLU goes to rows of
@@ -146,7 +146,9 @@ struct LogprobArgs {
   int32_t* top_index;      // [M][n_top], -1 behind the last logit that is a number
   float* top_logprob;
 };
-hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t ld, int M, int n, const LogprobArgs& a, hipStream_t s);
+// parts > 1: logits holds that many fp32 partials, `stride` elements apart, to be summed.
+hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t ld, int M, int n, int parts, int64_t stride, const LogprobArgs& a,
+                               hipStream_t s);
 // The same where the statistics of pieces of `width` columns are known (count to a row), the targets' logits among them; logits (16-byte
 // aligned, n and ld multiples of 4) are read for tokens only.
 hipError_t launch_logprob_pieces(const RowStatistics& st, int count, int width, const float* logits, int64_t ld, int M, int n,
