@@ -343,9 +343,9 @@ TDP_API int tdp_stage_timing_read(tdp_stage* st, float* ms /* host [8] */);
 typedef struct tdp_linear_i8 tdp_linear_i8;
 typedef struct {
   int32_t in_features;   /* K: a multiple of 8, at most 131072 */
-  int32_t out_features;  /* N: a multiple of 4; gated: of 8 */
+  int32_t out_features;  /* N: a multiple of 4; gated: of 8; at most 2^24 */
   int32_t gated;         /* 1: W = [W_gate | W_up] side by side, as in tdp_gemm_bf16: the result has N / 2 columns */
-  int32_t max_rows;      /* rows per call */
+  int32_t max_rows;      /* rows per call, at most 2^21 */
 } tdp_linear_i8_config;
 TDP_API int tdp_linear_i8_create(const tdp_linear_i8_config* cfg, tdp_linear_i8** out);
 TDP_API void tdp_linear_i8_destroy(tdp_linear_i8* h);
@@ -362,8 +362,9 @@ TDP_API int tdp_linear_i8_set_bias(tdp_linear_i8* h, const void* src, int32_t dt
 TDP_API int tdp_linear_i8_set_form(tdp_linear_i8* h, int32_t tile, int32_t splits);
 /* out[m] = y[m] (+ bias) (+ residual[m]), or silu(gate) * up if gated, for M <= max_rows rows (M = 0: nothing to do).
  *   x          dev, x_dtype, rows ld_x elements apart, 16-byte aligned: quantised by the call
- *   residual   dev, out_dtype, rows ld_residual elements apart, or null; gated: null.  May be out itself
- *   out        dev, out_dtype, rows ld_out elements apart: [M][N], gated [M][N / 2]; columns behind those are left as they are
+ *   residual   dev, out_dtype, rows ld_residual elements apart, or null; gated: null.  May be out itself (address and ld_out)
+ *   out        dev, out_dtype, rows ld_out elements apart: [M][N], gated [M][N / 2]; columns behind those are left as they are.  Shares
+ *              no element with x
  * TDP_F32 or TDP_BF16 each; out and residual aligned to four elements, row by row.  Sums, scales, bias and residual are joined in fp32
  * and rounded once. */
 TDP_API int tdp_linear_i8_run(tdp_linear_i8* h, const void* x, int32_t x_dtype, int64_t ld_x, int32_t M, const void* residual,

@@ -440,6 +440,7 @@ namespace {
 int fail_hip(hipError_t e, const char* what) {
   char buf[256];
   snprintf(buf, sizeof buf, "%s: %s", what, hipGetErrorString(e));
+  (void)hipGetLastError();  // (reported here; the next launch is not to be taken for the one that failed)
   return probe_fail(e == hipErrorOutOfMemory ? TDP_ENOMEM : TDP_EHIP, buf);
 }
 
@@ -508,7 +509,7 @@ int tdp_linear_i8_create(const tdp_linear_i8_config* cfg, tdp_linear_i8** out) {
   const int unit = cfg->gated ? 8 : 4;
   if (cfg->out_features < unit || cfg->out_features % unit || cfg->out_features > (1 << 24))
     return probe_fail(TDP_EINVAL, "out_features must be a multiple of 4 (gated: of 8), at most 2^24");
-  if (cfg->max_rows < 1 || cfg->max_rows > (1 << 24)) return probe_fail(TDP_EINVAL, "max_rows must be 1 .. 2^24");
+  if (cfg->max_rows < 1 || cfg->max_rows > (1 << 21)) return probe_fail(TDP_EINVAL, "max_rows must be 1 .. 2^21");
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return probe_fail(TDP_EHIP, "no HIP device");
   tdp_linear_i8* h = new (std::nothrow) tdp_linear_i8();

@@ -455,8 +455,9 @@ hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t 
   while ((1 << shift) < (vectors + threads - 1) / threads * per) ++shift;
   const bool nt = !top && (int64_t)M * n * (16 / per) >= (240ll << 20);
   const size_t lds = top && keep ? threads / 64 * sizeof(StagedUnits) : 0;
-#define TDP_ROWS(T, TOP, KEEP, NT, PARTS) \
-  logprob_rows_kernel<T, TOP, KEEP, NT, PARTS><<<M, threads, lds, s>>>((const T*)logits, ld, n, parts, stride, shift, a)
+#define TDP_ROWS(T, TOP, KEEP, NT, PARTS)                                                                                               \
+  logprob_rows_kernel<T, TOP, KEEP, NT, PARTS><<<rows, threads, lds, s>>>((const T*)logits + first * ld, ld, n, parts, stride, shift, \
+                                                                          a.from_row(first))
 #define TDP_ROWS_OF(T, PARTS)                                     \
   do {                                                            \
     if (top && keep) TDP_ROWS(T, true, true, false, PARTS);       \
@@ -466,9 +467,13 @@ hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t 
     else if (nt) TDP_ROWS(T, false, false, !PARTS, PARTS);        \
     else TDP_ROWS(T, false, false, false, PARTS);                 \
   } while (0)
-  if (parts > 1) TDP_ROWS_OF(float, true);
-  else if (logits_are_bf16) TDP_ROWS_OF(bf16, false);
-  else TDP_ROWS_OF(float, false);
+  const int64_t most = (1ll << 31) / threads;  // rows of a launch: its threads are counted in 32 bits
+  for (int64_t first = 0; first < M; first += most) {
+    const unsigned rows = (unsigned)(M - first < most ? M - first : most);
+    if (parts > 1) TDP_ROWS_OF(float, true);
+    else if (logits_are_bf16) TDP_ROWS_OF(bf16, false);
+    else TDP_ROWS_OF(float, false);
+  }
 #undef TDP_ROWS_OF
 #undef TDP_ROWS
   return hipGetLastError();

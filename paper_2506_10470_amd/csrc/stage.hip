@@ -842,22 +842,18 @@ void tdp_ends_destroy(tdp_ends* e) {
   delete e;
 }
 
-// The memory of the vocabulary projection in the form that is wanted, zeroed: what the form needs and does not have yet.  The other form's is
-// kept: a graph that was captured before still reads it.
-static hipError_t head_memory(tdp_ends* e, bool int8) {
-  const int64_t d = e->cfg.d_model, M = ((int64_t)e->cfg.max_tokens + 1) & ~1ll;
-  hipError_t err = hipSuccess;
+// What a vocabulary projection in 8 bits needs, from the first time on that one is set.  (The bf16 matrix stays: a graph that was captured
+// before still reads it.)
+static hipError_t int8_head_memory(tdp_ends* e) {
+  const int64_t M = ((int64_t)e->cfg.max_tokens + 1) & ~1ll;
+  hipError_t err = few_rows_setup();
   auto A = [&](auto** p, int64_t n) {
     if (!*p && err == hipSuccess) err = dev_alloc(p, n, true);
   };
-  if (!int8) {
-    A(&e->w_head, e->v_pad * d);
-  } else {
-    A(&e->head_codes, e->v_pad * e->d_pad);
-    A(&e->head_scale, e->v_pad);
-    A(&e->y_codes, M * e->d_pad);
-    A(&e->y_scale, e->cfg.max_tokens);
-  }
+  A(&e->head_codes, e->v_pad * e->d_pad);
+  A(&e->head_scale, e->v_pad);
+  A(&e->y_codes, M * e->d_pad);
+  A(&e->y_scale, e->cfg.max_tokens);
   return err;
 }
 int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dtype, int32_t mem, int64_t rows,
@@ -890,8 +886,7 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   const bool head = which == TDP_E_LM_HEAD || which == TDP_E_LM_HEAD_I8, int8 = which == TDP_E_LM_HEAD_I8;
   hipError_t err = hipSuccess;
   unsigned* column_max = nullptr;
-  if (head) err = head_memory(e, int8);
-  if (int8 && err == hipSuccess) err = few_rows_setup();
+  if (int8) err = int8_head_memory(e);
   if (int8 && err == hipSuccess) err = dev_alloc(&column_max, V, false);
   if (err == hipSuccess) {
     if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);

@@ -145,6 +145,10 @@ struct LogprobArgs {
   float *logprob, *entropy;
   int32_t* top_index;      // [M][n_top], -1 behind the last logit that is a number
   float* top_logprob;
+  LogprobArgs from_row(int64_t m) const {
+    auto on = [m](auto* p, int64_t width) { return p ? p + m * width : p; };
+    return {on(targets, 1), n_top, on(next_token, 1), on(logprob, 1), on(entropy, 1), on(top_index, n_top), on(top_logprob, n_top)};
+  }
 };
 // parts > 1: logits holds that many fp32 partials, `stride` elements apart, to be summed.
 hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t ld, int M, int n, int parts, int64_t stride, const LogprobArgs& a,

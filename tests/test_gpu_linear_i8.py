@@ -252,3 +252,55 @@ def test_calls_back_to_back_on_one_stream_share_the_scratch_in_order():
         outs = [lin.run(x) for x in xs]
         for x, out in zip(xs, outs):
             check(out, lin.exact(x))
+
+
+def test_a_creation_that_fails_leaves_nothing_behind():
+    """Weights of 2 TB: out of memory, and the next calls work"""
+    with pytest.raises(tdp.TdpError) as e:
+        tdp.tdp_linear_i8_create(tdp.LinearI8Config(131072, 1 << 24, 0, 1))
+    assert e.value.code == tdp.ENOMEM
+    with Linear(136, 64, 40).codes(1) as lin:
+        for M in (1, 40):
+            x = rows(M, 136, 2)
+            check(lin.run(x), lin.exact(x))
+
+
+def test_refusals():
+    with Linear(64, 32, 8).codes(1) as lin, Linear(64, 32, 8, True).codes(1) as gated:
+        x, out = rows(8, 64, 1), torch.zeros((8, 32), dtype=torch.bfloat16, device="cuda")
+        good = dict(x=x, x_dtype=tdp.BF16, ld_x=64, M=8, residual=None, ld_residual=0, out=out, out_dtype=tdp.BF16, ld_out=32)
+        run = lambda h, **kw: tdp.tdp_linear_i8_run(h, **{**good, **kw})
+        run(lin.h)
+        run(lin.h, M=0, x=None, out=None)
+        for bad in (dict(M=9), dict(M=-1), dict(x=None), dict(out=None), dict(x_dtype=2), dict(out_dtype=-1), dict(ld_x=63), dict(ld_x=65),
+                    dict(ld_x=56), dict(ld_out=31), dict(ld_out=28), dict(ld_out=34), dict(x=x.data_ptr() + 2), dict(out=out.data_ptr() + 2),
+                    dict(residual=out, ld_residual=30), dict(residual=out.data_ptr() + 4, ld_residual=32)):
+            with pytest.raises(tdp.TdpError) as e:
+                run(lin.h, **bad)
+            assert e.value.code == tdp.EINVAL, bad
+        with pytest.raises(tdp.TdpError):
+            run(gated.h, residual=out, ld_residual=32)
+        for h, call in ((lin.h, lambda: tdp.tdp_linear_i8_set_codes(lin.h, lin.w, lin.s, tdp.DEVICE, 32, 64)),
+                        (lin.h, lambda: tdp.tdp_linear_i8_set_codes(lin.h, lin.w, None, tdp.DEVICE, 64, 32)),
+                        (lin.h, lambda: tdp.tdp_linear_i8_set_weight(lin.h, x, 5, tdp.DEVICE, 64, 32)),
+                        (lin.h, lambda: tdp.tdp_linear_i8_set_weight(lin.h, x, tdp.BF16, 7, 64, 32)),
+                        (lin.h, lambda: tdp.tdp_linear_i8_set_bias(lin.h, lin.s, tdp.F32, tdp.DEVICE, 31)),
+                        (gated.h, lambda: tdp.tdp_linear_i8_set_bias(gated.h, gated.s, tdp.F32, tdp.DEVICE, 32)),
+                        (lin.h, lambda: tdp.tdp_linear_i8_set_form(lin.h, 11, 1)), (lin.h, lambda: tdp.tdp_linear_i8_set_form(lin.h, 14, 1)),
+                        (lin.h, lambda: tdp.tdp_linear_i8_set_form(lin.h, 1, 2)), (lin.h, lambda: tdp.tdp_linear_i8_set_form(lin.h, 1, 0))):
+            with pytest.raises(tdp.TdpError) as e:
+                call()
+            assert e.value.code == tdp.EINVAL
+        check(lin.run(x), lin.exact(x))
+
+
+def test_partials_beyond_the_workspace_are_refused_before_any_work():
+    """16 splits of 512 rows are 16 * 512 * 256 partials, and the workspace holds 8 * 512 * 256"""
+    with Linear(2048, 256, 512).codes(1) as lin:
+        tdp.tdp_linear_i8_set_form(lin.h, 3, 16)
+        out = torch.full((512, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+        with pytest.raises(tdp.TdpError) as e:
+            tdp.tdp_linear_i8_run(lin.h, rows(512, 2048, 1), tdp.BF16, 2048, 512, None, 0, out, tdp.BF16, 256)
+        assert e.value.code == tdp.EINVAL and (out == 7).all()
+        x = rows(200, 2048, 2)
+        check(lin.run(x), lin.exact(x))

@@ -123,6 +123,19 @@ def test_masks_ties_and_rows_without_a_distribution(n, n_top):
     check(call(zb.cuda(), tdp.BF16, len(z), n, n, targets, n_top), f64(zb), targets, n_top)
 
 
+def test_more_rows_than_a_launch_has_threads_for():
+    """70 million rows of four: 2^32 threads and more"""
+    M, n = 70_000_000, 4
+    z = torch.randn(M, n, device="cuda")
+    t = torch.randint(0, n, (M,), device="cuda", dtype=torch.int32)
+    lp, ix, tl = torch.empty(M, device="cuda"), torch.empty((M, 1), dtype=torch.int32, device="cuda"), torch.empty((M, 1), device="cuda")
+    tdp.tdp_logprob_rows(z, tdp.F32, M, n, n, t, 1, lp, None, ix, tl)
+    ref = torch.log_softmax(z, 1)
+    assert (lp - ref.gather(1, t.long()[:, None])[:, 0]).abs().max().item() <= 1e-4      # (both in fp32: 400 u of up to 20 each)
+    assert torch.equal(ix[:, 0].long(), z.argmax(1))
+    assert (tl[:, 0] - ref.max(1).values).abs().max().item() <= 1e-4
+
+
 def test_results_that_are_not_wanted_are_not_written_and_empty_calls_do_nothing():
     z = torch.randn(4, 50, device="cuda")
     en = torch.full((4,), 7.0, device="cuda")
@@ -199,6 +212,50 @@ def test_statistics_in_the_projections_epilogue_are_those_of_its_logits(M, vocab
             assert torch.equal(tok, tok2)
             lp2, en2, *_ = head.logprobs(x, M, t, 0, want_token=False)
             assert torch.equal(lp, lp2) and torch.equal(en, en2)
+
+
+def plan_of_head(M, vocab, d):
+    """How a bf16 vocabulary projection is made, with the workspace that an ends object for M rows has"""
+    padded = -(-vocab // 256) * 256
+    return tdp.tdp_gemm_plan(M, vocab, d, 0, False, 2 * min((M + 1) // 2 * 2, 512) * padded)
+
+
+# batches whose bf16 projection is made in tiles of every kind, unsplit; in chunks of K; and split
+BY_TILE = [(20, 8004, 64), (50, 32000, 128), (120, 32000, 320), (129, 8004, 64), (129, 16000, 64), (129, 32000, 64), (194, 16000, 64),
+           (194, 64000, 64), (324, 16000, 64), (324, 32000, 64), (454, 16000, 64), (454, 32000, 64), (1026, 8004, 64), (250, 32000, 512),
+           (33, 4100, 1152), (64, 8004, 2048), (100, 32000, 2048), (128, 2052, 4096), (16, 32000, 4096)]
+
+
+def test_the_batches_above_cover_the_kinds_of_tiles():
+    plans = [plan_of_head(*c) for c in BY_TILE]
+    assert {p["tile"] for p in plans if p["splits"] == 1 and not p["chunk_k"]} == {1, 3, 4, 5, 6, 7, 8, 9, 10, 12, 13}
+    assert {p["tile"] for p in plans if p["chunk_k"]} >= {11, 13} and any(p["splits"] > 1 for p in plans)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("M,vocab,d", BY_TILE)
+def test_statistics_of_every_kind_of_tile(M, vocab, d, int8):
+    """Against log-probabilities of the call's own logits in 64 bits, on the GPU.  (Tolerances as the oracle's, for logits whose spread R is
+    at most 40, D at most R: (2 R + 2 + 2 R + 72 + 200 + 2 ln n) u < 500 u and, of the entropy, (1 + R)(...) u.)"""
+    with Head(vocab, d, M, int8) as head:
+        x = head.rows(M, 5)
+        lg, _ = head.logits(x, M)
+        targets = np.random.default_rng(M).integers(0, vocab, M)
+        lp, en, *_ = head.logprobs(x, M, targets, 0, want_token=False)
+        z = lg.double()
+        assert (z.max() - z.min()).item() <= 40
+        ref = torch.log_softmax(z, 1)
+        at = torch.from_numpy(targets).cuda()[:, None]
+        entropy = -(ref.exp() * ref).sum(1)
+        R = 40
+        assert ((lp - ref.gather(1, at)[:, 0]).abs() <= (4 * R + 274 + 2 * np.log(vocab)) * U + 2 * U * R).all()
+        assert ((en - entropy).abs() <= (1 + R) * (4 * R + 300 + 2 * np.log(vocab)) * U).all()
+        # the tokens, where logits are stored, from the same tiles
+        lp2, en2, ix, tl, tok = head.logprobs(x, M, targets, 6)
+        assert torch.equal(lp, lp2) and torch.equal(en, en2)
+        top = lg.sort(stable=True, dim=1, descending=True)
+        assert torch.equal(ix.long(), top.indices[:, :6]) and torch.equal(tok.long(), top.indices[:, 0])
+        assert ((tl - ref.gather(1, top.indices[:, :6])).abs() <= 600 * U + 2 * U * R).all()
 
 
 @pytest.mark.parametrize("M", [1, 20, 300])
