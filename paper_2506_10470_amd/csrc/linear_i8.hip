@@ -136,6 +136,20 @@ hipError_t launch_quantise_rows(const void* x, int x_is_f32, int64_t ldx, const 
   return hipGetLastError();
 }
 
+// A wave's share of K in the two kernels below: `length` of `all` steps, contiguous, gone through in a circle from `turn` on.  (Shares start as far apart
+// as shares are long, and groups of weight rows 128 K bytes: where K is a power of two all waves of the chip would ask the same few
+// channels in step.  One row of 8192 x 8192 15.4 us without the turn.)
+struct Share {
+  int first, length, turn;
+  __device__ __forceinline__ Share(int all, int of, int which, int group) {
+    const int per = (all + of - 1) / of;
+    first = which * per;
+    length = max(0, min(per, all - first));
+    turn = length > 0 ? (which + group) % length : 0;
+  }
+  __device__ __forceinline__ int step(int i) const { return first + (i + turn >= length ? i + turn - length : i + turn); }
+};
+
 // ---- one row or two --------------------------------------------------------------------------------------------------------------
 // For a row or two a tile of 32 rows, its ring to fill, its partials to sum and two or three launches cost more than the weights are to
 // read.  One launch instead: every workgroup quantises the rows itself into LDS and streams weights through registers, the
@@ -143,7 +157,7 @@ hipError_t launch_quantise_rows(const void* x, int x_is_f32, int64_t ldx, const 
 // them at a time, and a lane multiplies its 16 codes with those of every row by v_dot4_i32_i8; the lanes of a weight row are added up
 // at the end.  Where there are too few weight rows for the chip the waves of a workgroup share K (slices).
 // Taken where one round of workgroups holds all weight rows (up to 16384 columns): one row of 256 x 256 3.4 us (tiles 5.8), 4096 x 4096
-// 6.3 (11.1), 5120 x 7168 9.4 (13.4), 28672 x 8192 41 (44: 5.8 TB/s); two rows 4.2, 8.0, 10.7, 42.7.  With more weight rows the
+// 6.3 (11.1), 5120 x 7168 9.8 (13.4), 8192 x 8192 13.9 (17.8), 28672 x 8192 43 (44: 5.4 TB/s); two rows 4.2, 8.3, 11.5, 15.2, 44.  With more weight rows the
 // tiles' longer runs of memory win: 4096 x 32000 26.0 (24.4), 8192 x 57344 in several turns 93 (72).  With four rows a workgroup's own quantisation costs what is
 // saved (4096 x 4096 12 and 11).
 constexpr int kFewRows = 2, kFewWaves = 8, kFewInFlight = 8, kFewLds = 128 * 1024;
@@ -161,12 +175,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const FewRowsP
   __shared__ int part[kFewWaves][MM][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int turns = (p.blocks_k + 3) / 4, k_lds = turns * 256;  // of 256 codes
-  const int slice = wave % p.slices, per = (turns + p.slices - 1) / p.slices, t0 = slice * per, t1 = min(t0 + per, turns);
+  const int slice = wave % p.slices;
   const int group = blockIdx.x * (kFewWaves / p.slices) + wave / p.slices;
   const int rr = (lane >> 2) & 3, kb = lane >> 4, c16 = (lane & 3) * 16;
   // this lane's weight row (past the last group: the last one's, for nothing)
   const int last = min(group, p.groups - 1), pair = last * 2 + (rr & 1);
   const int r = p.gated ? (pair / 32) * 64 + pair % 32 + (rr >> 1) * 32 : last * 4 + rr;
+  const Share share(turns, p.slices, slice, __builtin_amdgcn_readfirstlane(r >> kWeightGroupShift));  // (a wave's rows are of one group)
   const uint8_t* const row_base =
       (const uint8_t*)p.W + (int64_t)(r >> kWeightGroupShift) * (p.Kpad << kWeightGroupShift) + (r & ((1 << kWeightGroupShift) - 1)) * 64 + c16;
   i32x4 w[kFewInFlight];
@@ -226,7 +241,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const FewRowsP
   // (behind the loads of the rows: loads are waited for in order)
 #pragma unroll
   for (int u = 0; u < kFewInFlight; ++u)
-    if (t0 + u < t1) w[u] = fetch(t0 + u);
+    if (u < share.length) w[u] = fetch(share.step(u));
 #pragma unroll
   for (int m = 0; m < MM; ++m)
 #pragma unroll
@@ -281,18 +296,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const FewRowsP
   for (int m = 0; m < MM; ++m) acc[m] = 0;
   const uint8_t* const code = few_smem + kb * 64 + c16;
 #pragma unroll 1
-  for (int t = t0; t < t1; t += kFewInFlight) {
+  for (int i = 0; i < share.length; i += kFewInFlight) {
 #pragma unroll
     for (int u = 0; u < kFewInFlight; ++u) {
-      if (t + u >= t1) break;
+      if (i + u >= share.length) break;
+      const int t = share.step(i + u);
       const i32x4 v = w[u];
 #pragma unroll
       for (int m = 0; m < MM; ++m) {
-        const i32x4 a = *reinterpret_cast<const i32x4*>(code + m * k_lds + (t + u) * 256);
+        const i32x4 a = *reinterpret_cast<const i32x4*>(code + m * k_lds + t * 256);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[m] = __builtin_amdgcn_sdot4(v[i], a[i], acc[m], false);
+        for (int j = 0; j < 4; ++j) acc[m] = __builtin_amdgcn_sdot4(v[j], a[j], acc[m], false);
       }
-      if (t + u + kFewInFlight < t1) w[u] = fetch(t + u + kFewInFlight);
+      if (i + u + kFewInFlight < share.length) w[u] = fetch(share.step(i + u + kFewInFlight));
     }
   }
 #pragma unroll
@@ -361,6 +377,147 @@ hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
   while (p.slices < kFewWaves && p.groups * p.slices * 2 <= places * kFewWaves && turns >= 4 * p.slices) p.slices *= 2;
   const int blocks = (p.groups * p.slices + kFewWaves - 1) / kFewWaves;
   kFewKernels[a.M - 1][a.gain ? 2 : a.x_is_f32 ? 0 : 1]<<<blocks, 64 * kFewWaves, lds, s>>>(p);
+  return hipGetLastError();
+}
+
+// ---- a small batch ---------------------------------------------------------------------------------------------------------------
+// From rows that are quantised, up to 64 of them: a workgroup takes 16 or 32 weight rows, its eight waves an eighth of K each, and
+// adds up in LDS what split-K workgroups would leave as partials for a kernel behind them.  Weights and codes go straight from memory
+// to the registers of the MFMAs (a fragment of weights, 16 rows x 64 codes, is 1 KiB of memory in one piece; codes come from L2),
+// six k-steps ahead.
+// Taken where one round of workgroups holds all weight rows without leaving many CUs a share less, and where the codes that a CU reads
+// again stay below 512 KB (352 from 17 rows on): 3 rows of 4096 x 4096 7.9 us (tiles 11.3), 16 of 5120 x 7168 11.6 (15.5), 48 15.2 (16.9), 64
+// of 2048 x 2048 8.5 (11.2), 16 of 28672 x 8192 42 (46).  Beyond: 48 of 28672 x 8192 57 (49), 64 of 16384 x 1024 28 (20), 3 of 8192 x 10240,
+// 320 workgroups, 25 (21).  Level where K is 8192 (3 to 64 rows of 8192 x 8192 0.96 to 1.03 of the tiles' rate: groups of weight rows
+// begin 1 MB apart).
+constexpr int kSomeRows = 64, kSomeWaves = 8;
+struct SomeRowsParams {
+  const uint8_t *x, *W;  // codes: x_layout = layout_paired(Kpad / 2), layout_weights(Kpad / 2)
+  OperandLayout x_layout;
+  const float *x_scale, *w_scale, *bias;
+  const void* residual;
+  void* out;
+  int64_t Kpad, ldr, ldo;
+  int M, cols, gated, out_f32, steps;  // steps: k-blocks of 64
+};
+
+// MT tiles of 16 rows, NT of 16 weight rows (gated: gate and up rows of the same 16 columns)
+template <int MT, int NT>
+__global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(const SomeRowsParams p) {
+  constexpr int AHEAD = 6;
+  constexpr int PITCH = NT * 16 + 4;  // (a row of sums in LDS: 16-byte pieces, neighbouring rows in other banks)
+  __shared__ __attribute__((aligned(16))) int sums[kSomeWaves][MT * 16][PITCH];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kq = lane >> 4;
+  const int block = blockIdx.x;
+  auto weight_row = [&](int nt) {  // the first of tile nt
+    if (!p.gated) return (block * NT + nt) * 16;
+    const int j = block * 16;
+    return (j / 32) * 64 + j % 32 + nt * 32;
+  };
+  const Share share(p.steps, kSomeWaves, wave, weight_row(0) >> kWeightGroupShift);
+  const uint8_t *wp[NT], *xp[MT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = weight_row(nt) + l16;
+    wp[nt] = p.W + (int64_t)(r >> kWeightGroupShift) * (p.Kpad << kWeightGroupShift) + (r & ((1 << kWeightGroupShift) - 1)) * 64 + kq * 16;
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int m = min(mt * 16 + l16, p.M - 1);
+    xp[mt] = p.x + 2 * operand_offset(p.x_layout, m, kq * 8);
+  }
+  i32x4 w[AHEAD][NT], x[AHEAD][MT], acc[NT][MT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = i32x4{0, 0, 0, 0};
+  auto fetch = [&](int u, int i) {
+    const int t = share.step(i);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) w[u][nt] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wp[nt] + ((int64_t)t << (6 + kWeightGroupShift))));
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) x[u][mt] = *reinterpret_cast<const i32x4*>(xp[mt] + (int64_t)t * 128);
+  };
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (u < share.length) fetch(u, u);
+#pragma unroll 1
+  for (int i = 0; i < share.length; i += AHEAD) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (i + u >= share.length) break;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][nt], x[u][mt], acc[nt][mt], 0, 0, 0);
+      if (i + u + AHEAD < share.length) fetch(u, i + u + AHEAD);
+    }
+  }
+  // a lane holds weight rows kq * 4 .. + 3 of row l16
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<i32x4*>(&sums[wave][mt * 16 + l16][nt * 16 + kq * 4]) = acc[nt][mt];
+  __syncthreads();
+  const int quads = (p.gated ? 1 : NT) * 4, m = tid / quads, q = (tid - m * quads) * 4;  // (at most 512 quads)
+  const int col = (p.gated ? block * 16 : block * NT * 16) + q;
+  if (m >= p.M || col >= p.cols) return;
+  auto sum_at = [&](int n) {
+    i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kSomeWaves; ++i) s += *reinterpret_cast<const i32x4*>(&sums[i][m][n]);
+    const f32x4 scale = *reinterpret_cast<const f32x4*>(p.w_scale + weight_row(n >> 4) + (n & 15));
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * scale[e] * p.x_scale[m];
+    return v;
+  };
+  f32x4 v = sum_at(q);
+  if (NT == 2 && p.gated) {
+    const f32x4 up = sum_at(16 + q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = silu_f(v[e]) * up[e];
+  }
+  if (p.bias) v += *reinterpret_cast<const f32x4*>(p.bias + col);
+  if (p.out_f32) {
+    if (p.residual) v += *reinterpret_cast<const f32x4*>((const float*)p.residual + (int64_t)m * p.ldr + col);
+    *reinterpret_cast<f32x4*>((float*)p.out + (int64_t)m * p.ldo + col) = v;
+  } else {
+    bf16x4 o;
+    if (p.residual) {
+      const bf16x4 r = *reinterpret_cast<const bf16x4*>((const bf16*)p.residual + (int64_t)m * p.ldr + col);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += (float)r[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (bf16)v[e];
+    *reinterpret_cast<bf16x4*>((bf16*)p.out + (int64_t)m * p.ldo + col) = o;
+  }
+}
+
+// 32 weight rows to a workgroup where that leaves three quarters of the chip's CUs one.
+static bool some_rows_two(int gated, int cols) { return gated || (cols + 31) / 32 >= 192; }
+static int some_rows_grid(int gated, int cols) { return some_rows_two(gated, cols) && !gated ? (cols + 31) / 32 : (cols + 15) / 16; }
+bool some_rows_fit(int M, int64_t Kpad, int gated, int cols) {
+  const int grid = some_rows_grid(gated, cols), tiles = (M + 15) / 16;
+  if (M < 1 || M > kSomeRows || grid > 512 || (grid > 256 && grid < 360)) return false;
+  const int64_t codes = (int64_t)((grid + 255) / 256) * tiles * 16 * Kpad;  // of the rows, that a CU reads
+  return codes <= (tiles == 1 ? 512 : 352) * 1024;
+}
+
+hipError_t launch_some_rows(const SomeRowsParams& p, hipStream_t s) {
+  const bool two = some_rows_two(p.gated, p.cols);
+  const int grid = some_rows_grid(p.gated, p.cols);
+#define TDP_SOME(MT)                                                      \
+  (two ? some_rows_kernel<MT, 2><<<grid, 64 * kSomeWaves, 0, s>>>(p)      \
+       : some_rows_kernel<MT, 1><<<grid, 64 * kSomeWaves, 0, s>>>(p))
+  switch ((p.M + 15) / 16) {
+    case 1: TDP_SOME(1); break;
+    case 2: TDP_SOME(2); break;
+    case 3: TDP_SOME(3); break;
+    default: TDP_SOME(4); break;
+  }
+#undef TDP_SOME
   return hipGetLastError();
 }
 
@@ -623,7 +780,10 @@ int tdp_linear_i8_run(tdp_linear_i8* h, const void* x, int32_t x_dtype, int64_t 
     return e == hipSuccess ? TDP_OK : fail_hip(e, "tdp_linear_i8_run");
   }
   e = launch_quantise_rows(x, x_dtype == TDP_F32, ld_x, nullptr, 0.f, M, K, h->Kpad, h->codes, h->x_scale, s);
-  if (e == hipSuccess) {
+  if (e == hipSuccess && !h->form.tile && some_rows_fit(M, h->Kpad, h->cfg.gated, cols)) {
+    e = launch_some_rows({h->codes, h->w, layout_paired(h->Kpad / 2), h->x_scale, h->w_scale, h->has_bias ? h->bias : nullptr, residual, out, h->Kpad, ld_residual, ld_out, M, cols,
+                          h->cfg.gated, out_dtype == TDP_F32, (int)(h->Kpad / 64)}, s);
+  } else if (e == hipSuccess) {
     GemmArgs g;
     memset(&g, 0, sizeof(g));
     g.A = h->codes; g.a_layout = layout_paired(h->Kpad / 2); g.a_scale = h->x_scale;

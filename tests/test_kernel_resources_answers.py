@@ -29,8 +29,8 @@ def test_gemm_kinds(use, parameters, tiles, spilled):
 
 
 def test_row_kernels(use):
-    rows = {n: v for n, v in use.items() if re.search(r"logprob_(rows|pieces)_kernel|quantise_rows_kernel|few_rows_kernel", n)}
-    assert len(rows) == 16 + 2 + 3 + 6
+    rows = {n: v for n, v in use.items() if re.search(r"logprob_(rows|pieces)_kernel|quantise_rows_kernel|few_rows_kernel|some_rows_kernel", n)}
+    assert len(rows) == 16 + 2 + 3 + 6 + 8
     for name, (registers, spills, scratch) in rows.items():
         assert spills == 0 and scratch == 0, (name, spills, scratch)
         if "logprob_rows" in name:
