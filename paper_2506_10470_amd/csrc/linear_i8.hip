@@ -381,16 +381,17 @@ hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
 }
 
 // ---- a small batch ---------------------------------------------------------------------------------------------------------------
-// From rows that are quantised, up to 64 of them: a workgroup takes 16 or 32 weight rows, its eight waves an eighth of K each, and
+// From rows that are quantised: a workgroup takes up to 64 of them and 16 or 32 weight rows, its eight waves an eighth of K each, and
 // adds up in LDS what split-K workgroups would leave as partials for a kernel behind them.  Weights and codes go straight from memory
 // to the registers of the MFMAs (a fragment of weights, 16 rows x 64 codes, is 1 KiB of memory in one piece; codes come from L2),
 // six k-steps ahead.
 // Taken where one round of workgroups holds all weight rows without leaving many CUs a share less, and where the codes that a CU reads
 // again stay below 512 KB (352 from 17 rows on): 3 rows of 4096 x 4096 7.9 us (tiles 11.3), 16 of 5120 x 7168 11.6 (15.5), 48 15.2 (16.9), 64
 // of 2048 x 2048 8.5 (11.2), 16 of 28672 x 8192 42 (46).  Beyond: 48 of 28672 x 8192 57 (49), 64 of 16384 x 1024 28 (20), 3 of 8192 x 10240,
-// 320 workgroups, 25 (21).  Level where K is 8192 (3 to 64 rows of 8192 x 8192 0.96 to 1.03 of the tiles' rate: groups of weight rows
+// 320 workgroups, 25 (21).  More than 64 rows, in parts of 64, where 256 workgroups hold all: 128 of 4096 x 4096 13.3 (17.4), 200 of 2048 x 2048
+// 9.3 (11.5), 512 of 256 x 256 5.7 (6.9); 384 workgroups 333 of 2048 x 2048 14.4 (11.8).  Level where K is 8192 (3 to 64 rows of 8192 x 8192 0.96 to 1.03 of the tiles' rate: groups of weight rows
 // begin 1 MB apart).
-constexpr int kSomeRows = 64, kSomeWaves = 8;
+constexpr int kSomeRows = 64, kSomeWaves = 8;  // rows to a workgroup at most
 struct SomeRowsParams {
   const uint8_t *x, *W;  // codes: x_layout = layout_paired(Kpad / 2), layout_weights(Kpad / 2)
   OperandLayout x_layout;
@@ -408,7 +409,7 @@ __global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(const SomeRo
   constexpr int PITCH = NT * 16 + 4;  // (a row of sums in LDS: 16-byte pieces, neighbouring rows in other banks)
   __shared__ __attribute__((aligned(16))) int sums[kSomeWaves][MT * 16][PITCH];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, kq = lane >> 4;
-  const int block = blockIdx.x;
+  const int block = blockIdx.x, m0 = blockIdx.y * kSomeRows;
   auto weight_row = [&](int nt) {  // the first of tile nt
     if (!p.gated) return (block * NT + nt) * 16;
     const int j = block * 16;
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(const SomeRo
   }
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    const int m = min(mt * 16 + l16, p.M - 1);
+    const int m = min(m0 + mt * 16 + l16, p.M - 1);
     xp[mt] = p.x + 2 * operand_offset(p.x_layout, m, kq * 8);
   }
   i32x4 w[AHEAD][NT], x[AHEAD][MT], acc[NT][MT];
@@ -459,13 +460,13 @@ __global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(const SomeRo
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<i32x4*>(&sums[wave][mt * 16 + l16][nt * 16 + kq * 4]) = acc[nt][mt];
   __syncthreads();
-  const int quads = (p.gated ? 1 : NT) * 4, m = tid / quads, q = (tid - m * quads) * 4;  // (at most 512 quads)
+  const int quads = (p.gated ? 1 : NT) * 4, row = tid / quads, q = (tid - row * quads) * 4, m = m0 + row;  // (at most 512 quads)
   const int col = (p.gated ? block * 16 : block * NT * 16) + q;
-  if (m >= p.M || col >= p.cols) return;
+  if (row >= MT * 16 || m >= p.M || col >= p.cols) return;
   auto sum_at = [&](int n) {
     i32x4 s = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < kSomeWaves; ++i) s += *reinterpret_cast<const i32x4*>(&sums[i][m][n]);
+    for (int i = 0; i < kSomeWaves; ++i) s += *reinterpret_cast<const i32x4*>(&sums[i][row][n]);
     const f32x4 scale = *reinterpret_cast<const f32x4*>(p.w_scale + weight_row(n >> 4) + (n & 15));
     f32x4 v;
 #pragma unroll
@@ -496,22 +497,25 @@ __global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(const SomeRo
 }
 
 // 32 weight rows to a workgroup where that leaves three quarters of the chip's CUs one.
-static bool some_rows_two(int gated, int cols) { return gated || (cols + 31) / 32 >= 192; }
-static int some_rows_grid(int gated, int cols) { return some_rows_two(gated, cols) && !gated ? (cols + 31) / 32 : (cols + 15) / 16; }
+static int some_rows_parts(int M) { return (M + kSomeRows - 1) / kSomeRows; }
+static bool some_rows_two(int M, int gated, int cols) { return gated || (int64_t)((cols + 31) / 32) * some_rows_parts(M) >= 192; }
+static int some_rows_grid(int M, int gated, int cols) { return some_rows_two(M, gated, cols) && !gated ? (cols + 31) / 32 : (cols + 15) / 16; }
 bool some_rows_fit(int M, int64_t Kpad, int gated, int cols) {
-  const int grid = some_rows_grid(gated, cols), tiles = (M + 15) / 16;
-  if (M < 1 || M > kSomeRows || grid > 512 || (grid > 256 && grid < 360)) return false;
-  const int64_t codes = (int64_t)((grid + 255) / 256) * tiles * 16 * Kpad;  // of the rows, that a CU reads
+  if (M < 1) return false;
+  const int parts = some_rows_parts(M), grid = some_rows_grid(M, gated, cols), tiles = parts > 1 ? 4 : (M + 15) / 16;
+  const int64_t all = (int64_t)grid * parts;
+  if (all > (parts > 1 ? 256 : 512) || (all > 256 && all < 360)) return false;
+  const int64_t codes = (all + 255) / 256 * tiles * 16 * Kpad;  // of the rows, that a CU reads
   return codes <= (tiles == 1 ? 512 : 352) * 1024;
 }
 
 hipError_t launch_some_rows(const SomeRowsParams& p, hipStream_t s) {
-  const bool two = some_rows_two(p.gated, p.cols);
-  const int grid = some_rows_grid(p.gated, p.cols);
+  const bool two = some_rows_two(p.M, p.gated, p.cols);
+  const dim3 grid(some_rows_grid(p.M, p.gated, p.cols), some_rows_parts(p.M));
 #define TDP_SOME(MT)                                                      \
   (two ? some_rows_kernel<MT, 2><<<grid, 64 * kSomeWaves, 0, s>>>(p)      \
        : some_rows_kernel<MT, 1><<<grid, 64 * kSomeWaves, 0, s>>>(p))
-  switch ((p.M + 15) / 16) {
+  switch (p.M > kSomeRows ? 4 : (p.M + 15) / 16) {
     case 1: TDP_SOME(1); break;
     case 2: TDP_SOME(2); break;
     case 3: TDP_SOME(3); break;
