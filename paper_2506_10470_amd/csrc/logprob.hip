@@ -93,10 +93,11 @@ __device__ __forceinline__ float whole_sum(float v) {
 // Where many groups share the k-th maximum (a masked row with fewer tokens left than wanted: minus infinity, or whatever number stands for
 // it), only logits above it are listed; what is missing equals it, and is found by going through the row in order.  Where the
 // list overflows all the same (ties everywhere; large logits all in a few groups) logits above tau are listed from the whole
-// row, and tau is raised to the k-th largest listed as long as that overflows.
+// row, and tau is raised to the k-th largest listed if that overflows.  One such raise is enough for logits in no order; ones that ascend within a
+// few groups can gain a list's length at a time, so after kRaises of them tau becomes the k-th largest of the row, found by counting in 16 passes.
 // The code is kept short (loops, one place that lists): a workgroup has one row or two, and fetching instructions for the first
 // time is a good part of what a few hundred of them take.
-constexpr int kTopMost = 32, kListed = 512, kTied = 16, kStaged = 8;
+constexpr int kTopMost = 32, kListed = 512, kTied = 16, kStaged = 8, kRaises = 3;
 static_assert(kTopMost <= 64, "the bound is one of 64 maxima");
 
 struct RowShared {
@@ -207,7 +208,7 @@ __device__ __forceinline__ int select_top(const RowShared& rs, TopShared& sh, co
   int c = sh.listed;
   if (c > kListed) {
     above = true;
-    for (;;) {
+    for (int raises = 0;; ++raises) {
       __syncthreads();
       if (tid == 0) sh.listed = 0;
       __syncthreads();
@@ -216,10 +217,36 @@ __device__ __forceinline__ int select_top(const RowShared& rs, TopShared& sh, co
       __syncthreads();
       c = sh.listed;
       if (c <= kListed) break;
-      for (int i = tid; i < kListed; i += threads)
-        if (place_of(sh, sh.list[i], kListed) == k - 1) sh.tau = logit_of((unsigned)(sh.list[i] >> 32));  // (one entry)
-      __syncthreads();
-      tau = sh.tau;
+      if (raises < kRaises) {
+        for (int i = tid; i < kListed; i += threads)
+          if (place_of(sh, sh.list[i], kListed) == k - 1) sh.tau = logit_of((unsigned)(sh.list[i] >> 32));  // (one entry)
+        __syncthreads();
+        tau = sh.tau;
+      } else {
+        unsigned bound = 0;  // two bits of it at a time
+#pragma unroll 1
+        for (int bit = 30; bit >= 0; bit -= 2) {
+          int reached[3] = {0, 0, 0};
+          if (tid < 3) sh.wave_count[tid] = 0;
+#pragma unroll 1
+          for (int64_t i = tid; i < row.n; i += threads) {
+            const float z = row.at((int)i);
+            const unsigned order = z == z ? order_of(z) : 0u;
+#pragma unroll
+            for (int q = 0; q < 3; ++q) reached[q] += order >= (bound | (q + 1u) << bit);
+          }
+          __syncthreads();
+#pragma unroll
+          for (int q = 0; q < 3; ++q) atomicAdd(&sh.wave_count[q], reached[q]);
+          __syncthreads();
+          unsigned next = bound;
+#pragma unroll
+          for (int q = 0; q < 3; ++q) next = sh.wave_count[q] >= k ? bound | (q + 1u) << bit : next;
+          bound = next;
+          __syncthreads();
+        }
+        tau = logit_of(bound);
+      }
     }
   }
   if (c < k) {

@@ -123,6 +123,18 @@ def test_masks_ties_and_rows_without_a_distribution(n, n_top):
     check(call(zb.cuda(), tdp.BF16, len(z), n, n, targets, n_top), f64(zb), targets, n_top)
 
 
+@pytest.mark.parametrize("n,step,few", [(1 << 20, 1024, 16), ((1 << 20) + 3, 1024, 1), (131072, 1024, 31), (4096, 512, 100)])
+@pytest.mark.parametrize("n_top", [2, 20, 32])
+def test_large_logits_that_ascend_in_what_a_few_threads_read(n, step, few, n_top):
+    """All large logits in every step-th few vectors, larger and larger: no list of those at hand comes near the largest of the row."""
+    rng = np.random.default_rng(n + few)
+    large = (np.arange(n) // 4) % step < few
+    z = -1 - rng.random(n).astype(np.float32)
+    z[large] = np.float32(1) + np.arange(large.sum(), dtype=np.float32) * np.float32(2.0 ** -18)  # (exact: below 2^18 of them)
+    z = np.stack([z, np.where(large, z, np.float32(-np.inf)), -np.abs(z), np.where(rng.random(n) < 0.001, np.float32(np.nan), z)])
+    check(call(torch.from_numpy(z).cuda(), tdp.F32, len(z), n, n, None, n_top), z, None, n_top)
+
+
 def test_more_rows_than_a_launch_has_threads_for():
     """70 million rows of four: 2^32 threads and more"""
     M, n = 70_000_000, 4
