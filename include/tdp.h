@@ -339,7 +339,8 @@ TDP_API int tdp_stage_timing_read(tdp_stage* st, float* ms /* host [8] */);
  * infinity or a NaN has scale NaN, and with it its whole result; one of zeros has scale 0.
  * A tdp_linear_i8 owns the codes and scales of one weight matrix and scratch for max_rows rows.  It lives on the
  * device that is current when it is created, and calls on it need that device current.  Like a stage it must not be driven from two
- * streams at once, nor by two captured graphs that replay at once. */
+ * streams at once, nor by two captured graphs that replay at once.  Calls that set something wait for the device's work on all streams
+ * first, and return when they are done. */
 typedef struct tdp_linear_i8 tdp_linear_i8;
 typedef struct {
   int32_t in_features;   /* K: a multiple of 8, at most 131072 */

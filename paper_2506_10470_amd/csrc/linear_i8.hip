@@ -638,6 +638,8 @@ int set_weights(tdp_linear_i8* h, const void* src, int kind, const float* scales
   if (rows != K || cols != N) return probe_fail(TDP_EINVAL, "weight shape does not match the configuration");
   int rc = check_device(h);
   if (rc != TDP_OK) return rc;
+  hipError_t e = hipDeviceSynchronize();  // (a source may come from any stream, and calls on any may still read what is replaced)
+  if (e != hipSuccess) return fail_hip(e, "weight quantisation");
   const size_t size = kind == kWeightF32 ? 4 : kind == kWeightBf16 ? 2 : 1;
   const void *w = nullptr, *ws = nullptr;
   void *tmp = nullptr, *tmp_scales = nullptr;
@@ -646,7 +648,6 @@ int set_weights(tdp_linear_i8* h, const void* src, int kind, const float* scales
     if (tmp) (void)hipFree(tmp);
     return rc;
   }
-  hipError_t e = hipSuccess;
   for (int half = 0; half < (h->cfg.gated ? 2 : 1) && e == hipSuccess; ++half) {
     const int64_t cols_here = h->cfg.gated ? N / 2 : N, at = half * cols_here;
     e = launch_quantise_weights((const uint8_t*)w + at * size, kind, ws ? (const float*)ws + at : nullptr, K, cols_here, N,
@@ -732,10 +733,12 @@ int tdp_linear_i8_set_bias(tdp_linear_i8* h, const void* src, int32_t dtype, int
   if (n != h->cfg.out_features) return probe_fail(TDP_EINVAL, "bias length does not match the configuration");
   int rc = check_device(h);
   if (rc != TDP_OK) return rc;
+  hipError_t e = hipDeviceSynchronize();  // (as in set_weights)
+  if (e != hipSuccess) return fail_hip(e, "bias conversion");
   const void* dev = nullptr;
   void* tmp = nullptr;
   if ((rc = on_device(src, mem, (size_t)n * (dtype == TDP_F32 ? 4 : 2), &dev, &tmp)) != TDP_OK) return rc;
-  hipError_t e = launch_convert_vec(dev, dtype == TDP_F32, n, h->bias, 0);
+  e = launch_convert_vec(dev, dtype == TDP_F32, n, h->bias, 0);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (tmp) (void)hipFree(tmp);
   if (e != hipSuccess) return fail_hip(e, "bias conversion");

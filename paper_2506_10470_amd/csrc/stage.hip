@@ -886,7 +886,8 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   const bool head = which == TDP_E_LM_HEAD || which == TDP_E_LM_HEAD_I8, int8 = which == TDP_E_LM_HEAD_I8;
   hipError_t err = hipSuccess;
   unsigned* column_max = nullptr;
-  if (int8) err = int8_head_memory(e);
+  if (int8) err = hipDeviceSynchronize();  // (a source may come from any stream, and calls on any may still read what is replaced)
+  if (int8 && err == hipSuccess) err = int8_head_memory(e);
   if (int8 && err == hipSuccess) err = dev_alloc(&column_max, V, false);
   if (err == hipSuccess) {
     if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);

@@ -306,3 +306,29 @@ def test_partials_beyond_the_workspace_are_refused_before_any_work():
         assert e.value.code == tdp.EINVAL and (out == 7).all()
         x = rows(200, 2048, 2)
         check(lin.run(x), lin.exact(x))
+
+
+@pytest.mark.parametrize("what", ["codes", "weight"])
+def test_weights_that_another_stream_still_writes_are_waited_for(what):
+    K, N = 256, 512
+    with Linear(K, N, 4).codes(3) as lin:
+        w, s = torch.zeros_like(lin.w), torch.zeros_like(lin.s)
+        x = rows(4, K, 1)
+        lin.w, lin.s = -lin.w, 2 * lin.s
+        real = (lin.w.float() * lin.s).contiguous()
+        later = torch.zeros_like(real)
+        big = torch.zeros(1 << 28, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):  # some milliseconds
+                big += 1
+            w.copy_(lin.w)
+            s.copy_(lin.s)
+            later.copy_(real)
+        if what == "codes":
+            tdp.tdp_linear_i8_set_codes(lin.h, w, s, tdp.DEVICE, K, N)
+        else:
+            tdp.tdp_linear_i8_set_weight(lin.h, later, tdp.F32, tdp.DEVICE, K, N)
+            wc, ws = Q.quantise(real.cpu().numpy().T)
+            lin.w, lin.s = torch.from_numpy(wc.T.copy()), torch.from_numpy(ws)
+        check(lin.run(x), lin.exact(x))
