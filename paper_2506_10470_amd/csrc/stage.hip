@@ -856,6 +856,13 @@ static hipError_t int8_head_memory(tdp_ends* e) {
   A(&e->y_scale, e->cfg.max_tokens);
   return err;
 }
+
+static int check_ends_device(const tdp_ends* e) {
+  int dev = -1;
+  HIP_TRY(hipGetDevice(&dev));
+  return dev == e->device ? TDP_OK : fail(TDP_EINVAL, "the object was created on another device than the current one");
+}
+
 int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dtype, int32_t mem, int64_t rows,
                         int64_t cols) {
   if (!e || !src) return fail(TDP_EINVAL, "null ends object or source");
@@ -870,6 +877,11 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
     default: return fail(TDP_EINVAL, "unknown weight id");
   }
   if (rows != er || cols != ec) return fail(TDP_EINVAL, "weight shape does not match the configuration");
+  if (which == TDP_E_LM_HEAD_I8 && d > 131072) return fail(TDP_EINVAL, "a projection in 8-bit integers sums at most 131072 products");
+  if (which == TDP_E_LM_HEAD_I8) {
+    const int rc = check_ends_device(e);  // (its memory comes with the first call)
+    if (rc != TDP_OK) return rc;
+  }
   const size_t esz = dtype == TDP_F32 ? 4 : 2;
   const void* dsrc = src;
   void* tmp = nullptr;
@@ -981,7 +993,11 @@ int tdp_lm_head(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int
   int width = 0;
   const bool note = next_token && V >= kRowMaxColumns;
   const RowStatistics stats{e->row_max, e->row_sum, e->row_weighted, nullptr, nullptr, 1};
-  HIP_TRY(project_rows(e, hidden_in, n_rows_in, row_index, M, logits, note ? e->row_max : nullptr, note && e->int8 ? &stats : nullptr, &width, nullptr, s));
+  try {
+    HIP_TRY(project_rows(e, hidden_in, n_rows_in, row_index, M, logits, note ? e->row_max : nullptr, note && e->int8 ? &stats : nullptr, &width, nullptr, s));
+  } catch (...) {  // (the plan is remembered)
+    return fail(TDP_ENOMEM, "host allocation failed");
+  }
   if (next_token && width > 0)
     HIP_TRY(launch_argmax_pieces(e->row_max, (int)(e->v_pad / width), width, logits, V, M, V, next_token, s));
   else if (next_token)
@@ -1003,9 +1019,7 @@ int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, 
   int rc = check_head_call(e, hidden_in, n_rows_in, row_index, M, &done);
   if (rc == TDP_OK && e) rc = check_logprob_results(n_top, e->cfg.vocab_size, top_index, top_logprob);
   if (rc != TDP_OK || done) return rc;
-  int dev = -1;
-  HIP_TRY(hipGetDevice(&dev));
-  if (dev != e->device) return fail(TDP_EINVAL, "the object was created on another device than the current one");
+  if ((rc = check_ends_device(e)) != TDP_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
   const int V = e->cfg.vocab_size;
   // The projection's epilogue makes the statistics of every piece of a row from the logits in its registers; they are stored only for the

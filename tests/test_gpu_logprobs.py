@@ -354,3 +354,17 @@ def test_a_call_on_another_stream_waits_for_that_streams_work():
         w = z * 2
         got = call(w, tdp.F32, 64, 32000, 32000, None, 2, s)
     check(got, f64(w), None, 2)
+
+
+def test_an_8_bit_head_wider_than_its_sums_allow_is_refused():
+    """133184 products of 127 * 127 do not fit 32 bits"""
+    d = 133184
+    e = tdp.tdp_ends_create(tdp.EndsConfig(4, d, 1e-5, 1))
+    try:
+        w = torch.zeros((d, 4), device="cuda")
+        with pytest.raises(tdp.TdpError) as err:
+            tdp.tdp_ends_set_weight(e, tdp.E_LM_HEAD_I8, w, tdp.F32, tdp.DEVICE, d, 4)
+        assert err.value.code == tdp.EINVAL
+        tdp.tdp_ends_set_weight(e, tdp.E_LM_HEAD, w, tdp.F32, tdp.DEVICE, d, 4)
+    finally:
+        tdp.tdp_ends_destroy(e)
