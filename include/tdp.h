@@ -388,7 +388,8 @@ typedef struct {
 #define TDP_E_FINAL_NORM 1 /* [d_model, 1] */
 #define TDP_E_LM_HEAD 2    /* [d_model, vocab_size] row-major ([in, out] like every projection) */
 #define TDP_E_LM_HEAD_I8 3 /* the same, held in 8-bit integers with a scale for each token of the vocabulary (see tdp_linear_i8); the
-                              rows are then quantised behind the final norm.  d_model is at most 131072.  The projection is in the form that was set last. */
+                              rows are then quantised behind the final norm.  d_model is at most 131072.  The projection is in the
+                              form that was set last. */
 TDP_API int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out);
 TDP_API void tdp_ends_destroy(tdp_ends* e);
 /* src: host or device (mem), fp32 or bf16 (dtype); synchronous */

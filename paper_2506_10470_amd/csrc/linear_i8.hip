@@ -136,9 +136,9 @@ hipError_t launch_quantise_rows(const void* x, int x_is_f32, int64_t ldx, const 
   return hipGetLastError();
 }
 
-// A wave's share of K in the two kernels below: `length` of `all` steps, contiguous, gone through in a circle from `turn` on.  (Shares start as far apart
-// as shares are long, and groups of weight rows 128 K bytes: where K is a power of two all waves of the chip would ask the same few
-// channels in step.  One row of 8192 x 8192 15.4 us without the turn.)
+// A wave's share of K in the two kernels below: `length` of `all` steps, contiguous, gone through in a circle from `turn` on.  (Shares
+// start as far apart as shares are long, and groups of weight rows 128 K bytes: where K is a power of two all waves of the chip would ask
+// the same few channels in step.  One row of 8192 x 8192 15.4 us without the turn.)
 struct Share {
   int first, length, turn;
   __device__ __forceinline__ Share(int all, int of, int which, int group) {
@@ -152,14 +152,14 @@ struct Share {
 
 // ---- one row or two --------------------------------------------------------------------------------------------------------------
 // For a row or two a tile of 32 rows, its ring to fill, its partials to sum and two or three launches cost more than the weights are to
-// read.  One launch instead: every workgroup quantises the rows itself into LDS and streams weights through registers, the
-// first of them on their way meanwhile.  A wave takes four weight rows, in 1 KiB loads of four rows x four k-blocks of 64 codes, eight of
-// them at a time, and a lane multiplies its 16 codes with those of every row by v_dot4_i32_i8; the lanes of a weight row are added up
-// at the end.  Where there are too few weight rows for the chip the waves of a workgroup share K (slices).
-// Taken where one round of workgroups holds all weight rows (up to 16384 columns): one row of 256 x 256 3.4 us (tiles 5.8), 4096 x 4096
-// 6.3 (11.1), 5120 x 7168 9.8 (13.4), 8192 x 8192 13.9 (17.8), 28672 x 8192 43 (44: 5.4 TB/s); two rows 4.2, 8.3, 11.5, 15.2, 44.  With more weight rows the
-// tiles' longer runs of memory win: 4096 x 32000 26.0 (24.4), 8192 x 57344 in several turns 93 (72).  With four rows a workgroup's own quantisation costs what is
-// saved (4096 x 4096 12 and 11).
+// read.  One launch instead: every workgroup quantises the rows itself into LDS and streams weights through registers, the first of them
+// on their way meanwhile.  A wave takes four weight rows, in 1 KiB loads of four rows x four k-blocks of 64 codes, eight of them at a
+// time, and a lane multiplies its 16 codes with those of every row by v_dot4_i32_i8; the lanes of a weight row are added up at the end.
+// Where there are too few weight rows for the chip the waves of a workgroup share K (slices). Taken where one round of workgroups holds
+// all weight rows (up to 16384 columns): one row of 256 x 256 3.4 us (tiles 5.8), 4096 x 4096 6.3 (11.1), 5120 x 7168 9.8 (13.4), 8192 x
+// 8192 13.9 (17.8), 28672 x 8192 43 (44: 5.4 TB/s); two rows 4.2, 8.3, 11.5, 15.2, 44.  With more weight rows the tiles' longer runs of
+// memory win: 4096 x 32000 26.0 (24.4), 8192 x 57344 in several turns 93 (72).  With four rows a workgroup's own quantisation costs what
+// is saved (4096 x 4096 12 and 11).
 constexpr int kFewRows = 2, kFewWaves = 8, kFewInFlight = 8, kFewLds = 128 * 1024;
 struct FewRowsParams : FewRowsArgs {
   int slices, groups, blocks_k;  // waves that share K; groups of four weight rows; k-blocks
@@ -187,7 +187,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(const FewRowsP
   i32x4 w[kFewInFlight];
   auto fetch = [&](int t) {  // (a k-block behind the last: any, its codes are zero)
     const int block = 4 * t + kb;
-    return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(row_base + ((int64_t)(block < p.blocks_k ? block : 0) << (6 + kWeightGroupShift))));
+    const int64_t at = (int64_t)(block < p.blocks_k ? block : 0) << (6 + kWeightGroupShift);
+    return __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(row_base + at));
   };
   // the rows' largest magnitudes (and sums of squares), then their codes
   auto load8 = [&](int m, int c, float (&f)[8]) {
@@ -382,15 +383,14 @@ hipError_t launch_few_rows(const FewRowsArgs& a, hipStream_t s) {
 
 // ---- a small batch ---------------------------------------------------------------------------------------------------------------
 // From rows that are quantised: a workgroup takes up to 64 of them and 16 or 32 weight rows, its eight waves an eighth of K each, and
-// adds up in LDS what split-K workgroups would leave as partials for a kernel behind them.  Weights and codes go straight from memory
-// to the registers of the MFMAs (a fragment of weights, 16 rows x 64 codes, is 1 KiB of memory in one piece; codes come from L2),
-// six k-steps ahead.
-// Taken where one round of workgroups holds all weight rows without leaving many CUs a share less, and where the codes that a CU reads
-// again stay below 512 KB (352 from 17 rows on): 3 rows of 4096 x 4096 7.9 us (tiles 11.3), 16 of 5120 x 7168 11.6 (15.5), 48 15.2 (16.9), 64
-// of 2048 x 2048 8.5 (11.2), 16 of 28672 x 8192 42 (46).  Beyond: 48 of 28672 x 8192 57 (49), 64 of 16384 x 1024 28 (20), 3 of 8192 x 10240,
-// 320 workgroups, 25 (21).  More than 64 rows, in parts of 64, where 256 workgroups hold all: 128 of 4096 x 4096 13.3 (17.4), 200 of 2048 x 2048
-// 9.3 (11.5), 512 of 256 x 256 5.7 (6.9); 384 workgroups 333 of 2048 x 2048 14.4 (11.8).  Level where K is 8192 (3 to 64 rows of 8192 x 8192 0.96 to 1.03 of the tiles' rate: groups of weight rows
-// begin 1 MB apart).
+// adds up in LDS what split-K workgroups would leave as partials for a kernel behind them.  Weights and codes go straight from memory to
+// the registers of the MFMAs (a fragment of weights, 16 rows x 64 codes, is 1 KiB of memory in one piece; codes come from L2), six
+// k-steps ahead. Taken where one round of workgroups holds all weight rows without leaving many CUs a share less, and where the codes
+// that a CU reads again stay below 512 KB (352 from 17 rows on): 3 rows of 4096 x 4096 7.9 us (tiles 11.3), 16 of 5120 x 7168 11.6
+// (15.5), 48 15.2 (16.9), 64 of 2048 x 2048 8.5 (11.2), 16 of 28672 x 8192 42 (46).  Beyond: 48 of 28672 x 8192 57 (49), 64 of 16384 x
+// 1024 28 (20), 3 of 8192 x 10240, 320 workgroups, 25 (21).  More than 64 rows, in parts of 64, where 256 workgroups hold all: 128 of
+// 4096 x 4096 13.3 (17.4), 200 of 2048 x 2048 9.3 (11.5), 512 of 256 x 256 5.7 (6.9); 384 workgroups 333 of 2048 x 2048 14.4 (11.8).
+// Level where K is 8192 (3 to 64 rows of 8192 x 8192 0.96 to 1.03 of the tiles' rate: groups of weight rows begin 1 MB apart).
 constexpr int kSomeRows = 64, kSomeWaves = 8;  // rows to a workgroup at most
 struct SomeRowsParams {
   const uint8_t *x, *W;  // codes: x_layout = layout_paired(Kpad / 2), layout_weights(Kpad / 2)
@@ -435,7 +435,8 @@ __global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(const SomeRo
   auto fetch = [&](int u, int i) {
     const int t = share.step(i);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) w[u][nt] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wp[nt] + ((int64_t)t << (6 + kWeightGroupShift))));
+    for (int nt = 0; nt < NT; ++nt)
+      w[u][nt] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wp[nt] + ((int64_t)t << (6 + kWeightGroupShift))));
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) x[u][mt] = *reinterpret_cast<const i32x4*>(xp[mt] + (int64_t)t * 128);
   };
@@ -788,8 +789,8 @@ int tdp_linear_i8_run(tdp_linear_i8* h, const void* x, int32_t x_dtype, int64_t 
   }
   e = launch_quantise_rows(x, x_dtype == TDP_F32, ld_x, nullptr, 0.f, M, K, h->Kpad, h->codes, h->x_scale, s);
   if (e == hipSuccess && !h->form.tile && some_rows_fit(M, h->Kpad, h->cfg.gated, cols)) {
-    e = launch_some_rows({h->codes, h->w, layout_paired(h->Kpad / 2), h->x_scale, h->w_scale, h->has_bias ? h->bias : nullptr, residual, out, h->Kpad, ld_residual, ld_out, M, cols,
-                          h->cfg.gated, out_dtype == TDP_F32, (int)(h->Kpad / 64)}, s);
+    e = launch_some_rows({h->codes, h->w, layout_paired(h->Kpad / 2), h->x_scale, h->w_scale, h->has_bias ? h->bias : nullptr, residual,
+                          out, h->Kpad, ld_residual, ld_out, M, cols, h->cfg.gated, out_dtype == TDP_F32, (int)(h->Kpad / 64)}, s);
   } else if (e == hipSuccess) {
     GemmArgs g;
     memset(&g, 0, sizeof(g));

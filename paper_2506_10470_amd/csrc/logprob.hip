@@ -337,13 +337,14 @@ __device__ __forceinline__ void answer_row(const LogprobArgs& a, RowShared& rs, 
   }
   if constexpr (TOP) {
     const int k = max(a.n_top, a.next_token ? 1 : 0);
-    const int found = select_top(rs, *ts, row, l.max, k, edge, edge_at, turns, shift, largest_of, stage, element, [&](int place, int index, float value) {
+    auto write = [&](int place, int index, float value) {
       if (place == 0 && a.next_token) a.next_token[m] = index;
       if (place < a.n_top) {
         a.top_index[(int64_t)m * a.n_top + place] = index;
         a.top_logprob[(int64_t)m * a.n_top + place] = logprob(value);
       }
-    });
+    };
+    const int found = select_top(rs, *ts, row, l.max, k, edge, edge_at, turns, shift, largest_of, stage, element, write);
     for (int place = found + tid; place < a.n_top; place += blockDim.x) {  // (a row with fewer logits that are numbers)
       a.top_index[(int64_t)m * a.n_top + place] = -1;
       a.top_logprob[(int64_t)m * a.n_top + place] = NAN;
@@ -355,8 +356,8 @@ __device__ __forceinline__ void answer_row(const LogprobArgs& a, RowShared& rs, 
 // One workgroup per row, every logit read once.  A thread owns every `threads`-th vector.  KEEP: it has at most eight, and keeps them in
 // registers for the tokens; else any number, eight at a time, and those of threads whose largest logit is wanted are read again.
 constexpr int kInFlight = 8;
-// NT: the loads are marked non-temporal, from 240 MiB on, what the memory-side cache cannot hold beside anything else (1 GB of bf16: 180 -> 172 us, 263 MB of
-// fp32: 46 -> 41); below that logits that a projection has just written may still be there.
+// NT: the loads are marked non-temporal, from 240 MiB on, what the memory-side cache cannot hold beside anything else (1 GB of bf16: 180
+// -> 172 us, 263 MB of fp32: 46 -> 41); below that logits that a projection has just written may still be there.
 template <typename T, bool TOP, bool KEEP, bool NT, bool PARTS>
 __global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restrict__ logits, int64_t ld, int n, int parts, int64_t stride,
                                                                int shift, const LogprobArgs a) {

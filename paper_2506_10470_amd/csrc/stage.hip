@@ -905,7 +905,8 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
     if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);
     else if (which == TDP_E_FINAL_NORM) err = launch_convert_vec(dsrc, f32, d, e->gain, 0);
     else if (!int8) err = launch_repack(dsrc, f32, d, V, e->w_head, d, 0, 0, 0);
-    else err = launch_quantise_weights(dsrc, f32 ? kWeightF32 : kWeightBf16, nullptr, d, V, V, 0, e->head_codes, e->d_pad, e->head_scale, column_max, 0);
+    else err = launch_quantise_weights(dsrc, f32 ? kWeightF32 : kWeightBf16, nullptr, d, V, V, 0, e->head_codes, e->d_pad, e->head_scale,
+                                       column_max, 0);
   }
   if (err == hipSuccess) err = hipDeviceSynchronize();
   if (tmp) (void)hipFree(tmp);
@@ -994,7 +995,8 @@ int tdp_lm_head(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int
   const bool note = next_token && V >= kRowMaxColumns;
   const RowStatistics stats{e->row_max, e->row_sum, e->row_weighted, nullptr, nullptr, 1};
   try {
-    HIP_TRY(project_rows(e, hidden_in, n_rows_in, row_index, M, logits, note ? e->row_max : nullptr, note && e->int8 ? &stats : nullptr, &width, nullptr, s));
+    HIP_TRY(project_rows(e, hidden_in, n_rows_in, row_index, M, logits, note ? e->row_max : nullptr, note && e->int8 ? &stats : nullptr,
+                         &width, nullptr, s));
   } catch (...) {  // (the plan is remembered)
     return fail(TDP_ENOMEM, "host allocation failed");
   }

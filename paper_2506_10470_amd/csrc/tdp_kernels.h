@@ -166,8 +166,8 @@ hipError_t launch_logprob_pieces(const RowStatistics& st, int count, int width, 
 // 128), and scales [M].  With a gain (x bf16) the row is RMSNorm(x; gain): codes of x * gain, the scale times 1 / sqrt(mean x^2 + eps).
 hipError_t launch_quantise_rows(const void* x, int x_is_f32, int64_t ldx, const float* gain, float eps, int M, int K, int64_t Kpad,
                                 void* codes, float* scales, hipStream_t s);
-// The whole product of a row or two, quantised on the way, in one launch where few_rows_fit: as launch_quantise_rows and launch_gemm on integers, to the bit but
-// for the sum of squares of a norm.
+// The whole product of a row or two, quantised on the way, in one launch where few_rows_fit: as launch_quantise_rows and launch_gemm on
+// integers, to the bit but for the sum of squares of a norm.
 struct FewRowsArgs {
   const void* x;  // as in launch_quantise_rows
   int x_is_f32;

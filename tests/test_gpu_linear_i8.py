@@ -80,7 +80,8 @@ SIZES = [(1, 8, 4), (1, 256, 256), (2, 24, 8), (3, 128, 260), (5, 136, 100), (16
          # one row or two: K shared by all waves of a workgroup and by none, more LDS than half a CU's and the most there is, too many columns
          (1, 4096, 4096), (2, 28672, 1028), (1, 65536, 64), (2, 65536, 12), (1, 131072, 8), (2, 1000, 16384), (1, 136, 16388),
          # small batches: 32 weight rows to a workgroup, the last one partly filled; as many columns as a round holds, and more
-         (3, 4096, 7168), (20, 264, 6180), (48, 1000, 8188), (64, 136, 16380), (33, 520, 16388), (16, 8192, 10240), (65, 1000, 2044), (200, 2048, 2048), (512, 256, 256), (333, 688, 256), (129, 24, 4)]
+         (3, 4096, 7168), (20, 264, 6180), (48, 1000, 8188), (64, 136, 16380), (33, 520, 16388), (16, 8192, 10240),
+         (65, 1000, 2044), (200, 2048, 2048), (512, 256, 256), (333, 688, 256), (129, 24, 4)]
 
 
 @pytest.mark.parametrize("x_dtype,out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32), (torch.bfloat16, torch.float32),
@@ -103,7 +104,8 @@ def test_plain_bias_and_residual(M, K, N, x_dtype, out_dtype):
 
 
 @pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("M,K,F", [(1, 256, 688), (3, 8, 4), (17, 4096, 36), (48, 1000, 132), (2, 1000, 132), (1, 136, 260), (2, 4096, 8192), (33, 136, 8188), (64, 264, 8196), (100, 256, 688), (200, 512, 1376), (520, 136, 260)])
+@pytest.mark.parametrize("M,K,F", [(1, 256, 688), (3, 8, 4), (17, 4096, 36), (48, 1000, 132), (2, 1000, 132), (1, 136, 260), (2, 4096, 8192),
+                                   (33, 136, 8188), (64, 264, 8196), (100, 256, 688), (200, 512, 1376), (520, 136, 260)])
 def test_gated(M, K, F, out_dtype):
     with Linear(K, 2 * F, M, True).codes(M + F) as lin:
         x = rows(M, K, 3)
