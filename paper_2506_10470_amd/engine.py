@@ -6,10 +6,12 @@ allocation (the engine's job, Sec. 3.2.1), turns each event of the schedule into
 library (token embedding -> tdp_stage_prefill / tdp_stage_decode -> final norm + vocabulary
 projection + greedy selection) and keeps every request's tokens.  The pipeline clock of the
 schedule still comes from the profiles handed to the scheduler; the work itself is done by the HIP
-kernels, on the stream the caller names.  Host logic only: no arithmetic of the method lives here.
+kernels, on the stream the caller names, and so are the copies in front of them and behind them: ids and
+tables up, answers down.  Host logic only: no arithmetic of the method lives here.
 """
 from __future__ import annotations
 
+import functools
 from typing import Dict, List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -20,6 +22,16 @@ PAGE = 16
 
 class OutOfPages(RuntimeError):
     pass
+
+
+def _on_own_stream(method):
+    """The method with the worker's stream as the current one: torch's copies are then ordered with the kernels, and memory that it
+    takes and gives back is reused behind them."""
+    @functools.wraps(method)
+    def run(self, *args):
+        with torch.cuda.stream(self.torch_stream):
+            return method(self, *args)
+    return run
 
 
 class StageWorker:
@@ -33,10 +45,11 @@ class StageWorker:
     def __init__(self, tdp, stage: int, ends: int, d_model: int, num_pages: int, max_pages_per_seq: int,
                  max_batch: int, max_tokens: int, max_seqs: int, prompts: Sequence[Sequence[int]], stream=None,
                  check_tables: bool = False, logprobs: Optional[int] = None):
-        """logprobs: the log-probability of every generated token goes to self.logprobs[i] (beside
-        self.generated[i]), and of the `logprobs` likeliest tokens in its place (0: none) as (token, log-probability) pairs to
-        self.top[i].  check_tables: validate every call's block tables on the GPU first (tdp_stage_check_*): one
-        synchronisation per call, for runs that test the allocator rather than the throughput."""
+        """stream: a torch stream or its address (none: the current one); all of the worker's work is ordered on it, and what
+        the caller has queued elsewhere for these handles is the caller's to wait for.  logprobs: the log-probability of every
+        generated token goes to self.logprobs[i] (beside self.generated[i]), and of the `logprobs` likeliest tokens in its place
+        (0: none) as (token, log-probability) pairs to self.top[i].  check_tables: validate every call's block tables on the GPU
+        first (tdp_stage_check_*): one synchronisation per call, for runs that test the allocator rather than the throughput."""
         self.tdp, self.ends = tdp, ends
         self.stages = [stage] if isinstance(stage, int) else list(stage)
         self.stage = self.stages[0]
@@ -49,22 +62,26 @@ class StageWorker:
         self.pages: Dict[int, List[int]] = {}
         self.prompts = [list(map(int, p)) for p in prompts]
         self.generated: List[List[int]] = [[] for _ in prompts]
-        rows = max(max_batch, max_tokens, 1)
-        self.hidden = torch.empty((rows, d_model), dtype=torch.bfloat16, device="cuda")
-        self.hidden_out = torch.empty_like(self.hidden)
-        answers = max(max_batch, max_seqs, 1)
-        self.next_tok = torch.empty(answers, dtype=torch.int32, device="cuda")
         if logprobs is not None and not 0 <= logprobs <= tdp.MAX_TOP:
             raise ValueError("logprobs must be 0 .. %d" % tdp.MAX_TOP)
         self.n_top = logprobs
         self.logprobs: List[List[float]] = [[] for _ in prompts]
         self.top: List[List[List[Tuple[int, float]]]] = [[] for _ in prompts]
-        if logprobs is not None:
-            self.tok_logprob = torch.empty(answers, dtype=torch.float32, device="cuda")
-            self.top_index = torch.empty((answers, logprobs), dtype=torch.int32, device="cuda")
-            self.top_logprob = torch.empty((answers, logprobs), dtype=torch.float32, device="cuda")
+        self.torch_stream = (self.stream if isinstance(self.stream, torch.cuda.Stream)
+                             else torch.cuda.ExternalStream(getattr(self.stream, "cuda_stream", self.stream)))
+        self._buffers(max(max_batch, max_tokens, 1), max(max_batch, max_seqs, 1))
         self.stats = {"prefill_batches": 0, "prefill_tokens": 0, "decode_steps": 0, "decode_tokens": 0,
                       "released": 0, "evicted": 0, "min_free_pages": num_pages}
+
+    @_on_own_stream
+    def _buffers(self, rows: int, answers: int) -> None:
+        self.hidden = torch.empty((rows, self.d_model), dtype=torch.bfloat16, device="cuda")
+        self.hidden_out = torch.empty_like(self.hidden)
+        self.next_tok = torch.empty(answers, dtype=torch.int32, device="cuda")
+        if self.n_top is not None:
+            self.tok_logprob = torch.empty(answers, dtype=torch.float32, device="cuda")
+            self.top_index = torch.empty((answers, self.n_top), dtype=torch.int32, device="cuda")
+            self.top_logprob = torch.empty((answers, self.n_top), dtype=torch.float32, device="cuda")
 
     # ---- pages
     def _take(self, n: int) -> List[int]:
@@ -106,6 +123,7 @@ class StageWorker:
                 self.top[rid].append(list(zip(i, v)))
 
     # ---- the three events
+    @_on_own_stream
     def prefill(self, ids: List[int], lens: List[int]) -> None:
         n, total = len(ids), int(sum(lens))
         if n > self.max_seqs or total > self.max_tokens:
@@ -137,6 +155,7 @@ class StageWorker:
         self.stats["prefill_batches"] += 1
         self.stats["prefill_tokens"] += total
 
+    @_on_own_stream
     def decode(self, batch: int, ids: List[int], contexts: List[int]) -> None:
         n = len(ids)
         if n == 0:

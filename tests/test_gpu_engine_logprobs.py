@@ -78,3 +78,44 @@ def test_a_schedule_with_log_probabilities(int8, n_top):
 def test_the_worker_refuses_more_alternatives_than_there_can_be():
     with pytest.raises(ValueError):
         StageWorker(tdp, 1, 1, 64, 4, 4, 4, 4, 4, [[1]], logprobs=tdp.MAX_TOP + 1)
+
+
+def run_on(stream, sh, reqs, prompts, busy):
+    """A schedule with log-probabilities on `stream` (None: the current one), behind `busy` milliseconds or so of other work on it."""
+    capacity, budget = 600, 128
+    max_len = max(r[0] + r[1] for r in reqs) + 1
+    max_pps = (max_len + 15) // 16 + 1
+    num_pages = (capacity + 15) // 16 + len(reqs)
+    rows = max(budget, max_len, len(reqs))
+    with Stage(tdp, sh, num_pages, len(reqs), rows, len(reqs), max_pps) as st, Ends(sh, VOCAB, rows) as ends:
+        st.poison()
+        big = torch.zeros(1 << 28, device="cuda")
+        torch.cuda.synchronize()
+        w = StageWorker(tdp, st.h, ends.h, sh.d_model, num_pages, max_pps, len(reqs), rows, len(reqs), prompts, stream=stream, logprobs=3)
+        late = []
+
+        def behind_other_work(event):
+            def call(*args):
+                with torch.cuda.stream(w.torch_stream):
+                    for _ in range(busy):
+                        big.add_(1)
+                event(*args)
+                late.append(torch.cuda.current_stream() == before)
+            return call
+        before = torch.cuda.current_stream()
+        w.prefill, w.decode = behind_other_work(w.prefill), behind_other_work(w.decode)
+        w.run(L, L.SimConfig(2, capacity, budget, 1, 1, 1, 1), reqs, DEC, PRE, events_cap=1 << 20)
+        torch.cuda.synchronize()
+        assert late and all(late)          # (the caller's current stream is what it was)
+        return w.generated, w.logprobs, w.top
+
+
+def test_a_worker_on_a_stream_of_its_own_gives_the_same_answers():
+    """The same calls on the same shapes: the same bits.  Ids, tables and answers are copied while the worker's stream is milliseconds
+    behind the caller's, and the caller's current stream, on which copies would not wait, is another."""
+    sh = W.SHAPES["tiny_gqa"]
+    reqs, prompts = make_requests(12, 9)
+    want = run_on(None, sh, reqs, prompts, 0)
+    side = torch.cuda.Stream()
+    assert run_on(side, sh, reqs, prompts, 4) == want
+    assert run_on(side.cuda_stream, sh, reqs, prompts, 4) == want          # by its address
