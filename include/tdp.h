@@ -392,7 +392,9 @@ typedef struct {
                               form that was set last. */
 TDP_API int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out);
 TDP_API void tdp_ends_destroy(tdp_ends* e);
-/* src: host or device (mem), fp32 or bf16 (dtype); synchronous */
+/* src: host or device (mem), fp32 or bf16 (dtype).  Waits for the device's work on all streams first (a source may be written by any,
+ * and calls on any may still read the weight that is replaced), and returns when it is done.  The device on which the object was created has
+ * to be current. */
 TDP_API int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dtype, int32_t mem,
                                 int64_t rows, int64_t cols);
 /* hidden_out[m][:] = embedding[token_ids[m]][:].  token_ids dev int32 [M]; hidden_out dev bf16

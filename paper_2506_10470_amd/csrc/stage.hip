@@ -878,10 +878,9 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   }
   if (rows != er || cols != ec) return fail(TDP_EINVAL, "weight shape does not match the configuration");
   if (which == TDP_E_LM_HEAD_I8 && d > 131072) return fail(TDP_EINVAL, "a projection in 8-bit integers sums at most 131072 products");
-  if (which == TDP_E_LM_HEAD_I8) {
-    const int rc = check_ends_device(e);  // (its memory comes with the first call)
-    if (rc != TDP_OK) return rc;
-  }
+  const int rc = check_ends_device(e);
+  if (rc != TDP_OK) return rc;
+  HIP_TRY(hipDeviceSynchronize());  // (a source may come from any stream, and calls on any may still read what is replaced)
   const size_t esz = dtype == TDP_F32 ? 4 : 2;
   const void* dsrc = src;
   void* tmp = nullptr;
@@ -898,8 +897,7 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   const bool head = which == TDP_E_LM_HEAD || which == TDP_E_LM_HEAD_I8, int8 = which == TDP_E_LM_HEAD_I8;
   hipError_t err = hipSuccess;
   unsigned* column_max = nullptr;
-  if (int8) err = hipDeviceSynchronize();  // (a source may come from any stream, and calls on any may still read what is replaced)
-  if (int8 && err == hipSuccess) err = int8_head_memory(e);
+  if (int8) err = int8_head_memory(e);
   if (int8 && err == hipSuccess) err = dev_alloc(&column_max, V, false);
   if (err == hipSuccess) {
     if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);

@@ -252,3 +252,46 @@ def test_infinite_logits(M):
         up = x[:, 0].float().cpu().numpy() > 0
         assert np.isneginf(lg[up][:, columns]).all() and np.isnan(lg[2, columns]).all()
         assert np.array_equal(toks.cpu().numpy(), E.greedy_tokens(np.where(np.isnan(lg), -np.inf, lg)))
+
+
+def some_milliseconds_of_work():
+    big = torch.zeros(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+
+    def on_the_current_stream():
+        for _ in range(20):
+            big.add_(1)
+    return on_the_current_stream
+
+
+# weight, its shape, and the logit and the embedding that follow from ones everywhere but this weight of twos, d_model 64
+@pytest.mark.parametrize("which,rows,cols,logit,embedding", [(tdp.E_FINAL_NORM, 64, 1, 128.0, 1.0), (tdp.E_LM_HEAD, 64, 1000, 128.0, 1.0),
+                                                             (tdp.E_EMBEDDING, 1000, 64, 64.0, 2.0)])
+def test_weights_that_another_stream_still_writes_are_waited_for(which, rows, cols, logit, embedding):
+    """And a call that another stream has yet to make still sees the weight that is replaced behind it."""
+    vocab, d, M = 1000, 64, 4
+    e = tdp.tdp_ends_create(tdp.EndsConfig(vocab, d, 0.0, M))
+    try:
+        for w, shape in ((tdp.E_FINAL_NORM, (d, 1)), (tdp.E_LM_HEAD, (d, vocab)), (tdp.E_EMBEDDING, (vocab, d))):
+            tdp.tdp_ends_set_weight(e, w, torch.ones(shape, device="cuda"), tdp.F32, tdp.DEVICE, *shape)
+        x, ids = torch.ones(M, d, device="cuda", dtype=torch.bfloat16), i32([0] * M)
+
+        def outputs(stream):
+            lg, hid = torch.zeros(M, vocab, device="cuda"), torch.zeros(M, d, device="cuda", dtype=torch.bfloat16)
+            torch.cuda.synchronize()
+            return lg, hid, lambda: (tdp.tdp_lm_head(e, x, M, None, M, lg, None, stream), tdp.tdp_embed_tokens(e, ids, M, hid, stream))
+        side = torch.cuda.Stream()
+        source, busy = torch.zeros(rows, cols, device="cuda"), some_milliseconds_of_work()
+        lg1, hid1, before = outputs(side)
+        lg2, hid2, after = outputs(None)
+        with torch.cuda.stream(side):
+            busy()
+            source.fill_(2.0)
+        before()
+        tdp.tdp_ends_set_weight(e, which, source, tdp.F32, tdp.DEVICE, rows, cols)
+        after()
+        torch.cuda.synchronize()
+        assert (lg1 == 64).all() and (hid1 == 1).all()      # (the norm of ones is ones, in bf16 too)
+        assert (lg2 == logit).all() and (hid2 == embedding).all()
+    finally:
+        tdp.tdp_ends_destroy(e)
