@@ -128,7 +128,8 @@ TDP_API void tdp_stage_destroy(tdp_stage* st);
  * [rows] with cols = 1, of type `dtype` (TDP_F32 or TDP_BF16; fp32 is rounded to bf16 with
  * round-to-nearest-even, gains are kept in fp32), living where `mem` says (TDP_HOST or
  * TDP_DEVICE).  The library repacks it once into its own MFMA-friendly layout; `src` is not
- * referenced after the call returns (the call synchronises).  Shapes must match the config.
+ * referenced after the call returns.  The call waits for the device's work on all streams before it reads
+ * the source and replaces the weight, and for its own before it returns.  Shapes must match the config.
  */
 TDP_API int tdp_stage_set_weight(tdp_stage* st, int32_t layer, int32_t which, const void* src,
                          int32_t dtype, int32_t mem, int64_t rows, int64_t cols);

@@ -456,6 +456,7 @@ int tdp_stage_set_weight(tdp_stage* st, int32_t layer, int32_t which, const void
              (long long)ec, (long long)rows, (long long)cols);
     return fail(TDP_EINVAL, buf);
   }
+  HIP_TRY(hipDeviceSynchronize());  // (a source may come from any stream, and calls on any may still read what is replaced)
   const size_t esz = dtype == TDP_F32 ? 4 : 2;
   const void* dsrc = src;
   void* tmp = nullptr;

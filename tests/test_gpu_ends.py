@@ -295,3 +295,41 @@ def test_weights_that_another_stream_still_writes_are_waited_for(which, rows, co
         assert (lg2 == logit).all() and (hid2 == embedding).all()
     finally:
         tdp.tdp_ends_destroy(e)
+
+
+def test_a_stages_weights_that_another_stream_still_writes_are_waited_for():
+    """A gain and a matrix, and a step that another stream has yet to make when they are replaced."""
+    sh = W.SHAPES["tiny"]
+    with Stage(tdp, sh, 8, 4, 32, 4, 4) as st:
+        st.poison()
+        x = torch.randn(20, sh.d_model, device="cuda").to(torch.bfloat16)
+        cu, table = i32([0, 20]), i32([[0, 1, 2, 3]])
+
+        def prefill(stream=None):
+            y = torch.zeros_like(x)
+            torch.cuda.synchronize()
+            return y, lambda: tdp.tdp_stage_prefill(st.h, x, cu, table, 1, 20, y, stream)
+        sources = {name: (2 * W.weight(sh, 0, name, device="cuda", dtype=torch.bfloat16)).contiguous() for name in ("g_attn", "wd")}
+
+        def replace(name, source):
+            tdp.tdp_stage_set_weight(st.h, 0, tdp.WEIGHT_IDS[name], source, tdp.BF16, tdp.DEVICE, source.shape[0],
+                                     source.shape[1] if source.dim() == 2 else 1)
+        old, call = prefill()
+        call()
+        for name, source in sources.items():
+            late, side, busy = torch.zeros_like(source), torch.cuda.Stream(), some_milliseconds_of_work()
+            y1, before = prefill(side)
+            y2, after = prefill()
+            with torch.cuda.stream(side):
+                busy()
+                late.copy_(source)
+            before()
+            replace(name, late)
+            after()
+            torch.cuda.synchronize()
+            assert torch.equal(y1, old), name
+            replace(name, source)
+            old, call = prefill()
+            call()
+            torch.cuda.synchronize()
+            assert torch.equal(y2, old) and not torch.equal(y1, old), name
