@@ -378,7 +378,8 @@ TDP_API int tdp_linear_i8_run(tdp_linear_i8* h, const void* x, int32_t x_dtype, 
  * 4.1 and Table 2): the token-embedding lookup, and the final RMSNorm + vocabulary projection +
  * greedy selection.  A tdp_ends owns the embedding table (bf16 [vocab, d_model]), the final norm
  * gain (fp32) and the vocabulary projection (bf16, repacked once), plus scratch for max_tokens rows.
- * vocab_size must be a multiple of 4, d_model a multiple of 64. */
+ * vocab_size must be a multiple of 4, d_model a multiple of 64.
+ * The object lives on the device that is current when it is created, and calls on it need that device current (TDP_EINVAL). */
 typedef struct tdp_ends tdp_ends;
 typedef struct {
   int32_t vocab_size, d_model;
@@ -394,8 +395,7 @@ typedef struct {
 TDP_API int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out);
 TDP_API void tdp_ends_destroy(tdp_ends* e);
 /* src: host or device (mem), fp32 or bf16 (dtype).  Waits for the device's work on all streams first (a source may be written by any,
- * and calls on any may still read the weight that is replaced), and returns when it is done.  The device on which the object was created has
- * to be current. */
+ * and calls on any may still read the weight that is replaced), and returns when it is done. */
 TDP_API int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dtype, int32_t mem,
                                 int64_t rows, int64_t cols);
 /* hidden_out[m][:] = embedding[token_ids[m]][:].  token_ids dev int32 [M]; hidden_out dev bf16
@@ -430,8 +430,7 @@ TDP_API int tdp_logprob_rows(const void* logits, int32_t dtype, int32_t M, int32
 /* The same behind tdp_lm_head's norm and projection (hidden_in, n_rows_in, row_index, M as there), with the greedy token as
  * there in next_token (dev int32 [M] or null): what an engine answers a token with, or, with a prompt's own next tokens as targets, what
  * scores it.  Logits are kept inside, and where neither next_token nor n_top asks for tokens they are not stored at all.  An ends
- * object must not be driven from two streams at once, nor by two captured graphs that replay at once; this call needs the device
- * current on which it was created. */
+ * object must not be driven from two streams at once, nor by two captured graphs that replay at once. */
 TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, const int32_t* row_index, int32_t M,
                                  const int32_t* targets, int32_t n_top, int32_t* next_token, float* logprob, float* entropy,
                                  int32_t* top_index, float* top_logprob, void* stream);

@@ -920,6 +920,8 @@ int tdp_embed_tokens(tdp_ends* e, const int32_t* token_ids, int32_t M, void* hid
   if (M < 0) return fail(TDP_EINVAL, "negative size");
   if (M == 0) return TDP_OK;
   if (!token_ids || !hidden_out) return fail(TDP_EINVAL, "null pointer");
+  const int rc = check_ends_device(e);
+  if (rc != TDP_OK) return rc;
   HIP_TRY(launch_gather_rows(e->table, e->cfg.d_model, e->cfg.vocab_size, token_ids, M, e->cfg.d_model, hidden_out,
                              e->cfg.d_model, (hipStream_t)stream));
   return TDP_OK;
@@ -935,7 +937,7 @@ static int check_head_call(const tdp_ends* e, const void* hidden_in, int32_t n_r
   if (!hidden_in || n_rows_in < 1) return fail(TDP_EINVAL, "no input rows");
   if (!row_index && M > n_rows_in) return fail(TDP_EINVAL, "M exceeds the input rows");
   *done = false;
-  return TDP_OK;
+  return check_ends_device(e);
 }
 
 // Final norm and vocabulary projection: logits[m] = RMSNorm(x; gain) * W_head, fp32 [M][V].  The norm hands its rows on in bf16, or as codes to a
@@ -1020,7 +1022,6 @@ int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_rows_in, 
   int rc = check_head_call(e, hidden_in, n_rows_in, row_index, M, &done);
   if (rc == TDP_OK && e) rc = check_logprob_results(n_top, e->cfg.vocab_size, top_index, top_logprob);
   if (rc != TDP_OK || done) return rc;
-  if ((rc = check_ends_device(e)) != TDP_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
   const int V = e->cfg.vocab_size;
   // The projection's epilogue makes the statistics of every piece of a row from the logits in its registers; they are stored only for the

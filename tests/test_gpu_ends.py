@@ -333,3 +333,19 @@ def test_a_stages_weights_that_another_stream_still_writes_are_waited_for():
             call()
             torch.cuda.synchronize()
             assert torch.equal(y2, old) and not torch.equal(y1, old), name
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="one device")
+def test_calls_with_another_device_current_are_refused():
+    sh = W.SHAPES["tiny"]
+    with Ends(sh, 64, 4) as e:
+        x, tok, lp = torch.zeros(4, sh.d_model, device="cuda", dtype=torch.bfloat16), i32([0] * 4), torch.zeros(4, device="cuda")
+        calls = [lambda: tdp.tdp_embed_tokens(e.h, tok, 4, x), lambda: tdp.tdp_lm_head(e.h, x, 4, None, 4, None, tok),
+                 lambda: tdp.tdp_lm_head_logprobs(e.h, x, 4, None, 4, None, 0, tok, lp, None, None, None),
+                 lambda: tdp.tdp_ends_set_weight(e.h, tdp.E_FINAL_NORM, e.gain, tdp.F32, tdp.DEVICE, sh.d_model, 1)]
+        for call in calls:
+            call()
+            torch.cuda.synchronize()
+            with torch.cuda.device(1), pytest.raises(tdp.TdpError) as err:
+                call()
+            assert err.value.code == tdp.EINVAL
