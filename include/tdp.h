@@ -257,6 +257,13 @@ TDP_API int tdp_gemm_plan(int32_t M, int32_t N, int32_t K, int32_t epilogue, int
                           int32_t* plan);
 
 /*
+ * Diagnostic, on the host alone: the same for a product of 8-bit integers (tdp_linear_i8_run, TDP_E_LM_HEAD_I8) that is made in
+ * tiles; the kernels for small batches have none.  workspace_elems: of a tdp_linear_i8 as tdp_linear_i8_set_form says, of a tdp_ends
+ * 2 * min(rows, 512) * N, rows = max_tokens rounded up to 2 and N to 256.  plan (host int32 [4]): as the first four there.
+ */
+TDP_API int tdp_gemm_plan_i8(int32_t M, int32_t N, int32_t K, int32_t gated, int64_t workspace_elems, int32_t* plan);
+
+/*
  * Diagnostic: tdp_gemm_bf16 made in exactly one way, so that every kernel variant can be tested whatever
  * the plan would take: tile = a tile number of tdp_gemm_plan (from 1), splits = the split-K factor (one
  * that leaves no split empty), chunk_k = 0 or a multiple of 64: a workgroup sums its K range in chunks of

@@ -640,6 +640,20 @@ int tdp_gemm_plan(int32_t M, int32_t N, int32_t K, int32_t epilogue, int32_t def
   return TDP_OK;
 }
 
+int tdp_gemm_plan_i8(int32_t M, int32_t N, int32_t K, int32_t gated, int64_t workspace_elems, int32_t* plan) {
+  if (M < 1 || N < 4 || N % 4 || K < 8 || K % 8 || K > 131072) return fail(TDP_EINVAL, "bad shape of a product of integers");
+  if (gated != 0 && gated != 1) return fail(TDP_EINVAL, "gated must be 0 or 1");
+  if (gated && N % 8) return fail(TDP_EINVAL, "the gated epilogue needs N = 2 F with F a multiple of 4");
+  if (workspace_elems < 0) return fail(TDP_EINVAL, "negative workspace");
+  if (!plan) return fail(TDP_EINVAL, "null pointer");
+  const int64_t Npad = gated ? 2 * round_up(N / 2, 128) : round_up(N, 256);
+  const GemmPlan p = gemm_plan({M, 0, 0, gated ? EPI_SWIGLU : EPI_STORE, false, true, Npad, round_up(K, 128) / 2, workspace_elems});
+  plan[0] = p.tile;
+  gemm_tile_size(p.tile, plan + 1, plan + 2);
+  plan[3] = p.splits;
+  return TDP_OK;
+}
+
 // one projection from a row-major weight matrix; form.tile = 0: planned, with tile and splits as far as they are given
 static int gemm_bf16(const char* what, const void* A, const void* W, const void* residual, void* out, int M, int N, int K,
                      int epilogue, int tile, int splits, GemmPlan form, hipStream_t s) {

@@ -77,6 +77,7 @@ _SIGS = {
     "tdp_stage_set_layer_range": (C.c_int, [_vp, _i32, _i32]),
     "tdp_stage_set_decode_span": (C.c_int, [_vp, _i32]),
     "tdp_gemm_plan": (C.c_int, [_i32, _i32, _i32, _i32, _i32, _i64, C.POINTER(_i32)]),
+    "tdp_gemm_plan_i8": (C.c_int, [_i32, _i32, _i32, _i32, _i64, C.POINTER(_i32)]),
     "tdp_gemm_bf16": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
     "tdp_gemm_bf16_form": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
     "tdp_gemm_bf16_static": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp]),
@@ -206,6 +207,13 @@ def tdp_gemm_plan(M, N, K, epilogue=0, deferred=False, workspace_elems=None) -> 
     p = (_i32 * 5)()
     _check(lib.tdp_gemm_plan(M, N, K, epilogue, int(bool(deferred)), workspace_elems, p))
     return dict(zip(("tile", "rows", "weight_rows", "splits", "chunk_k"), p))
+
+
+def tdp_gemm_plan_i8(M, N, K, gated=False, workspace_elems=0) -> dict:
+    """How a product of 8-bit integers is made in tiles."""
+    p = (_i32 * 4)()
+    _check(lib.tdp_gemm_plan_i8(M, N, K, int(bool(gated)), workspace_elems, p))
+    return dict(zip(("tile", "rows", "weight_rows", "splits"), p))
 
 
 def tdp_gemm_bf16(A, W, residual, out, M, N, K, epilogue=0, tile=0, splits=0, stream=None) -> None:

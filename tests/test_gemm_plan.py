@@ -35,3 +35,28 @@ def test_plan_entry_rejects_bad_arguments():
         assert P(M, N, K, epi, deferred, ws, out) == tdp.EINVAL
     assert P(1, 64, 64, 0, 0, 0, None) == tdp.EINVAL
     assert P(1, 64, 64, 0, 0, 0, out) == tdp.OK and out[3] == 1 and out[4] == 0
+
+
+def test_plan_of_integers_rejects_bad_arguments():
+    import ctypes as C
+    out = (C.c_int32 * 5)(7, 7, 7, 7, 7)
+    P = tdp.lib.tdp_gemm_plan_i8
+    for M, N, K, gated, ws in [(0, 64, 64, 0, 0), (1, 66, 64, 0, 0), (1, 64, 12, 0, 0), (1, 64, 0, 0, 0), (1, 64, 131080, 0, 0),
+                               (1, 68, 64, 1, 0), (1, 64, 64, 2, 0), (1, 64, 64, 0, -1)]:
+        assert P(M, N, K, gated, ws, out) == tdp.EINVAL
+    assert P(1, 64, 64, 0, 0, None) == tdp.EINVAL
+    assert list(out) == [7] * 5
+    assert P(1, 64, 64, 0, 0, out) == tdp.OK and out[3] == 1 and out[4] == 7
+
+
+@pytest.mark.parametrize("M,N,K,gated", [(1, 4, 8, 0), (48, 7168, 5120, 0), (512, 57344, 8192, 1), (300, 2056, 136, 1), (8191, 8192, 131072, 0)])
+def test_plan_of_integers_fits_the_workspace_and_leaves_no_split_empty(M, N, K, gated):
+    """Of a tdp_linear_i8: 8 * min(rows, 512) * N, N rounded up"""
+    padded = 2 * (-(-N // 2 // 128) * 128) if gated else -(-N // 256) * 256
+    ws = min(8 * min(M + M % 2, 512) * padded, 64 << 20)
+    p = tdp.tdp_gemm_plan_i8(M, N, K, gated, ws)
+    assert p["tile"] in set(range(1, 14)) - {11} and p["rows"] % 32 == 0 and p["weight_rows"] in (128, 256)
+    assert p["splits"] == 1 or p["splits"] * M * padded <= ws
+    k_tiles = -(-K // 128)
+    per = -(-k_tiles // p["splits"])
+    assert (p["splits"] - 1) * per < k_tiles

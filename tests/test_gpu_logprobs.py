@@ -319,6 +319,32 @@ def test_rows_by_index_and_hidden_states_that_are_not_numbers(int8):
         assert (ix[5] == -1).all() and tok[5] == 0
 
 
+# the tile that the batches above leave out, and vocabularies that take it
+MORE_BY_TILE = [(65, 50304, 64), (100, 64000, 320), (128, 128256, 64), (3, 4100, 2048)]
+
+
+def plan_of_int8_head(M, vocab, d):
+    padded = -(-vocab // 256) * 256
+    return tdp.tdp_gemm_plan_i8(M, vocab, d, False, 2 * min((M + 1) // 2 * 2, 512) * padded)
+
+
+def test_all_batches_cover_every_kind_of_tile_of_both_heads():
+    cases = BY_TILE + MORE_BY_TILE
+    bf16, int8 = [plan_of_head(*c) for c in cases], [plan_of_int8_head(*c) for c in cases]
+    every = set(range(1, 14)) - {11}      # (11 sums in chunks: of bf16 alone)
+    assert {p["tile"] for p in bf16 if p["splits"] == 1 and not p["chunk_k"]} == every
+    assert {p["tile"] for p in int8 if p["splits"] == 1} == every
+    assert any(p["splits"] > 1 for p in int8) and any(p["splits"] > 1 for p in bf16)
+    for vocab in (50304, 64000, 100000, 128256):      # ordinary decode batches
+        assert {plan_of_int8_head(M, vocab, 4096)["tile"] for M in (65, 100, 128)} == {2}
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("M,vocab,d", MORE_BY_TILE)
+def test_statistics_of_the_other_kinds_of_tiles(M, vocab, d, int8):
+    test_statistics_of_every_kind_of_tile(M, vocab, d, int8)
+
+
 def test_captured_calls_replay_with_new_contents():
     """Both calls in one graph on a stream of their own, replayed with other logits and hidden states, with eager work between."""
     M, vocab, d = 40, 4100, 256
