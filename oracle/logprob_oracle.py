@@ -34,18 +34,22 @@ def answer(z: np.ndarray, targets, n_top: int):
             np.array([r[3] for r in rows]).reshape(len(rows), n_top))
 
 
-def tolerance(z: np.ndarray):
+def tolerance(z: np.ndarray, links=None):
     """(of a log-probability, of an entropy) per row: what an fp32 evaluation relative to the row's maximum can be off by.
 
     With u = 2^-24, d = z - m (spread R = max |d| over what e^d does not turn into 0 in fp32, at most 104), D = sum p |d|:
     a difference is off by u |d|, the product with log2 e in front of the exponential by u |d| of its result, the exponential by 2 u:
     (2 |d| + 2) u per term, (2 D + 2) u of s.  Moving a partial sum to a larger maximum: (2 |change| + 3) u, the changes of a chain add up
-    to R, at most 24 links (turns of a thread that raise its maximum, 6 + 4 exchanges, pieces): (2 R + 72) u.  Additions: up to 200 in a
-    chain: 200 u.  ln s: off by that sum (relative error of s) and 2 u |ln s| of its own.
+    to R, in `links` links: 6 + 4 exchanges and the turns of a thread that raise its maximum, of 32768 logits or more, or of 16384 of a
+    projection in pieces; up to 14 of those, a row of 229376, it is 24 links and (2 R + 72) u, beyond that as many more as a row
+    that rises from turn to turn has.  (A row known to rise less often may give its own number.)
+    Additions: up to 200 u.  A row's are 64 in a turn, 2 u for the sum of the turns, which is kept in two numbers, and 10 exchanges; a
+    projection's 34, one for 16384 columns (of 2 million: 128) and 10.  ln s: off by that sum (relative error of s) and 2 u |ln s| of its own.
     t = sum e^d d: the same per term and 2 u more, weighted with |d| <= R: (2 R + 4) u D, and the chain's and the additions' share of D."""
     u = 2.0 ** -24
     out = []
     for r in np.asarray(z, dtype=np.float64):
+        chain = 3 * (links or 10 + max(14, -(-len(r) // 16384)))
         r = r[np.isfinite(r)]
         if not len(r):
             out.append((0.0, 0.0))
@@ -54,6 +58,6 @@ def tolerance(z: np.ndarray):
         e = np.exp(d)
         D = np.sum(e * -d) / e.sum()
         R = min(104.0, -d.min())
-        s = (2 * D + 2 + 2 * R + 72 + 200 + 2 * abs(np.log(e.sum()))) * u
-        out.append((s, s + (2 * R + 4) * D * u + (2 * R + 72 + 200 + 4) * D * u + 2 * u * D))
+        s = (2 * D + 2 + 2 * R + chain + 200 + 2 * abs(np.log(e.sum()))) * u
+        out.append((s, s + (2 * R + 4) * D * u + (2 * R + chain + 200 + 4) * D * u + 2 * u * D))
     return np.array(out).reshape(-1, 2).T

@@ -61,6 +61,19 @@ struct LogitRow {
   }
 };
 
+// A sum of many terms in two numbers: `lost` takes what an addition to `sum` rounds off, exactly where |v| <= |sum|.  (Terms of one sign,
+// 64 at most: elsewhere the sum at least doubles, so that what such additions round off is in all twice the last one's, u of the sum.)
+__device__ __forceinline__ void add_in_two(float& sum, float& lost, float v) {
+  const float s = sum + v;
+  lost += v - (s - sum);
+  sum = s;
+}
+__device__ __forceinline__ void take_in(LogSum& l, float& lost_sum, float& lost_weighted) {
+  l.sum += lost_sum;
+  l.weighted += lost_weighted;
+  lost_sum = lost_weighted = 0.f;
+}
+
 // ---- sums over lanes -------------------------------------------------------------------------------------------------------------
 // A lane's value joined with those of the lanes in front of it, by DPP: behind step i lane l holds what lanes l - 2^i + 1 .. l of its row of 16
 // have, then rows 1 and 3, 2 and 3 take what stands in front of them.  Lane 63 holds all.
@@ -354,7 +367,9 @@ __device__ __forceinline__ void answer_row(const LogprobArgs& a, RowShared& rs, 
 }
 
 // One workgroup per row, every logit read once.  A thread owns every `threads`-th vector.  KEEP: it has at most eight, and keeps them in
-// registers for the tokens; else any number, eight at a time, and those of threads whose largest logit is wanted are read again.
+// registers for the tokens; else any number, eight at a time, and those of threads whose largest logit is wanted are read again.  What
+// each turn of eight adds is then a sum of its own, and the sum of those is kept in two numbers: in one, like terms are rounded
+// alike time after time, and a row of 2^24 was off by 2e-4 where a chain of 64 is by 4e-6 at most.
 constexpr int kInFlight = 8;
 // NT: the loads are marked non-temporal, from 240 MiB on, what the memory-side cache cannot hold beside anything else (1 GB of bf16: 180
 // -> 172 us, 263 MB of fp32: 46 -> 41); below that logits that a projection has just written may still be there.
@@ -378,6 +393,7 @@ __global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restri
     row.stride = stride;
   }
   LogSum l = no_logits();
+  float lost_sum = 0.f, lost_weighted = 0.f;
   u32x4 z[kInFlight];
   auto fetch = [&](int v0) {
 #pragma unroll
@@ -389,17 +405,27 @@ __global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restri
     for (int u = 0; u < kInFlight; ++u)
 #pragma unroll
       for (int e = 0; e < kPer; ++e) max = fmaxf(max, Row::value(z[u], e));
-    if (max > l.max) raise(l, max);
+    if (max > l.max) {
+      if constexpr (!KEEP) take_in(l, lost_sum, lost_weighted);
+      raise(l, max);
+    }
     const float r = reference_of(max);
+    LogSum turn{max, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       if (u > 0 && v0 - tid + u * threads >= row.body) break;  // (the same for all threads)
       asm volatile("" : "+v"(z[u]));  // (bf16: converted here again, the values of two passes would not fit)
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) add_distance(l, Row::value(z[u], e) - r);
+      for (int e = 0; e < kPer; ++e) add_distance(turn, Row::value(z[u], e) - r);
+    }
+    if constexpr (KEEP) {
+      l = turn;
+    } else {
+      add_in_two(l.sum, lost_sum, turn.sum);
+      add_in_two(l.weighted, lost_weighted, turn.weighted);
     }
   };
-  const int target = a.targets ? a.targets[m] : -1, edge_at = row.edge(tid);
+  const int target = a.targets ? a.targets[m] : -1, edge_at = PARTS ? -1 : row.edge(tid);  // (PARTS: rows of whole vectors)
   if constexpr (KEEP) fetch(tid);
   const bool has_target = target >= 0 && target < n;
   const float target_logit = has_target ? row.at(target) : 0.f, edge = edge_at >= 0 ? row.at(edge_at) : -INFINITY;
@@ -411,6 +437,7 @@ __global__ __launch_bounds__(1024, 8) void logprob_rows_kernel(const T* __restri
       fetch(v0);
       add(v0);
     }
+    take_in(l, lost_sum, lost_weighted);
   }
   const float own_max = l.max;
   if (edge_at >= 0) {

@@ -150,7 +150,7 @@ struct LogprobArgs {
     return {on(targets, 1), n_top, on(next_token, 1), on(logprob, 1), on(entropy, 1), on(top_index, n_top), on(top_logprob, n_top)};
   }
 };
-// parts > 1: logits holds that many fp32 partials, `stride` elements apart, to be summed.
+// parts > 1: logits holds that many fp32 partials, `stride` elements apart, to be summed (16-byte aligned; n, ld and stride multiples of 4).
 hipError_t launch_logprob_rows(const void* logits, int logits_are_bf16, int64_t ld, int M, int n, int parts, int64_t stride, const LogprobArgs& a,
                                hipStream_t s);
 // The same where the statistics of pieces of `width` columns are known (count to a row), the targets' logits among them; logits (16-byte

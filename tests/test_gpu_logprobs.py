@@ -135,6 +135,30 @@ def test_large_logits_that_ascend_in_what_a_few_threads_read(n, step, few, n_top
     check(call(torch.from_numpy(z).cuda(), tdp.F32, len(z), n, n, None, n_top), z, None, n_top)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,value", [((1 << 22) + 5, -1.0), ((1 << 22) + 5, -1.5), ((1 << 24) + 5, -0.25), ((1 << 24) + 5, -0.5),
+                                     ((1 << 24) + 5, -1.0)])
+def test_sums_of_many_like_terms(n, value, dtype):
+    """Every thread's first logits are the row's largest, all others alike: added one by one to a single fp32 number, each of them would
+    be rounded the same way as long as that number has the same exponent, thousands of times.  Maxima rise once: 24 links."""
+    top = 8192
+    for shift in (0, 3):
+        z = torch.full((shift + n,), value, dtype=dtype, device="cuda")
+        z[:shift + top] = 0
+        lp, en, _, _ = call(z[shift:], tdp.F32 if dtype == torch.float32 else tdp.BF16, 1, n, n, [n - 1], 0)
+        e = np.exp(value)
+        s = top + (n - top) * e
+        of_log, of_entropy = L.tolerance(f64(z[shift:])[None], links=24)
+        near(lp, [value - np.log(s)], of_log)
+        near(en, [np.log(s) - (n - top) * e * value / s], of_entropy)
+
+
+def test_a_long_row_that_rises_to_its_end():
+    n = (1 << 22) + 3
+    z = (np.arange(n) * 2.0 ** -18).astype(np.float32)[None]      # (exact)
+    check(call(torch.from_numpy(z).cuda(), tdp.F32, 1, n, n, [n - 9], 2), z, [n - 9], 2)
+
+
 def test_more_rows_than_a_launch_has_threads_for():
     """70 million rows of four: 2^32 threads and more"""
     M, n = 70_000_000, 4
