@@ -4,6 +4,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <string>
 #include <vector>
 
@@ -798,11 +799,12 @@ struct tdp_ends {
   uint16_t* rows = nullptr;    // bf16 [max_tokens][d]: gathered input rows
   uint16_t* y = nullptr;       // bf16, pair-interleaved [max_tokens ^ 2][d]: normalised rows
   float* logits = nullptr;     // [max_tokens][vocab]
-  float* row_max = nullptr;    // the largest logit of every piece of a row
-  float *row_sum = nullptr, *row_weighted = nullptr, *target_logit = nullptr;  // the rest of RowStatistics
-  int device = 0;
+  // Split-K partials, or what a projection that is not split notes of every piece of a row: one call makes the one or the other.
   float* ws = nullptr;
-  int64_t ws_elems = 0;
+  int64_t ws_elems = 0;        // that partials may take
+  float *row_max = nullptr, *row_sum = nullptr, *row_weighted = nullptr;  // in ws: [max_tokens][v_pad / kRowMaxWidth] each
+  float* target_logit = nullptr;  // [max_tokens]: the rest of RowStatistics
+  int device = 0;
 };
 
 int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out) {
@@ -831,12 +833,15 @@ int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out) {
   A(&e->rows, M * d, true);
   A(&e->y, M * d, true);
   A(&e->logits, (int64_t)cfg->max_tokens * V, false);
-  A(&e->row_max, (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth), false);
-  A(&e->row_sum, (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth), false);
-  A(&e->row_weighted, (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth), false);
   A(&e->target_logit, cfg->max_tokens, false);
   e->ws_elems = 2 * (M < 512 ? M : 512) * e->v_pad;
-  A(&e->ws, e->ws_elems, false);
+  const int64_t noted = (int64_t)cfg->max_tokens * (e->v_pad / kRowMaxWidth);
+  A(&e->ws, std::max(e->ws_elems, 3 * noted), false);
+  if (err == hipSuccess) {
+    e->row_max = e->ws;
+    e->row_sum = e->ws + noted;
+    e->row_weighted = e->ws + 2 * noted;
+  }
   if (err == hipSuccess) err = hipDeviceSynchronize();
   if (err != hipSuccess) {
     const int code = fail_hip(err, "tdp_ends_create");
@@ -850,8 +855,8 @@ int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out) {
 void tdp_ends_destroy(tdp_ends* e) {
   if (!e) return;
   (void)hipDeviceSynchronize();
-  void* ptrs[] = {e->table, e->gain, e->w_head, e->rows, e->y, e->logits, e->row_max, e->row_sum, e->row_weighted, e->target_logit, e->ws,
-                  e->head_codes, e->head_scale, e->y_codes, e->y_scale};
+  void* ptrs[] = {e->table, e->gain, e->w_head, e->rows, e->y, e->logits, e->target_logit, e->ws, e->head_codes, e->head_scale, e->y_codes,
+                  e->y_scale};
   for (void* p : ptrs)
     if (p) (void)hipFree(p);
   delete e;

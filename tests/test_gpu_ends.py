@@ -349,3 +349,47 @@ def test_calls_with_another_device_current_are_refused():
             with torch.cuda.device(1), pytest.raises(tdp.TdpError) as err:
                 call()
             assert err.value.code == tdp.EINVAL
+
+
+def memory_taken(make):
+    """(what make returns, MiB of the device's memory that it has taken)"""
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    made = make()
+    torch.cuda.synchronize()
+    return made, (before - torch.cuda.mem_get_info()[0]) / 2 ** 20
+
+
+@pytest.mark.parametrize("vocab,rows", [(32000, 8192), (2048, 60000)])
+def test_an_ends_object_takes_no_memory_for_what_it_notes_of_logits(vocab, rows):
+    """Table, projection, two buffers of rows, logits and partials, each rounded up by the allocator (2 MiB); the notes, three numbers
+    for 64 logits, are where partials would be, unless a call of very many rows has more of them than partials."""
+    d = 64
+    e, mib = memory_taken(lambda: tdp.tdp_ends_create(tdp.EndsConfig(vocab, d, 1e-5, rows)))
+    tdp.tdp_ends_destroy(e)
+    behind = max(2 * 512 * vocab * 4, 3 * rows * (vocab // 64) * 4)
+    named = (2 * vocab * d * 2 + 2 * rows * d * 2 + rows * vocab * 4 + behind) / 2 ** 20
+    assert mib <= named + 2 * 9, (mib, named)      # (less where small buffers come from memory that the runtime holds already)
+
+
+def test_more_rows_than_partials_have_room_for():
+    """Notes of 60000 rows take more than a split's partials of 512: every row's token is its logits' largest, and its log-probability
+    that of the same call on fewer rows."""
+    vocab, d, M = 4096, 64, 60000
+    e = tdp.tdp_ends_create(tdp.EndsConfig(vocab, d, 1e-5, M))
+    try:
+        g = torch.Generator(device="cuda").manual_seed(1)
+        w = (torch.randn(d, vocab, generator=g, device="cuda") / 8).to(torch.bfloat16)
+        x = torch.randn(M, d, generator=g, device="cuda").to(torch.bfloat16)
+        tdp.tdp_ends_set_weight(e, tdp.E_FINAL_NORM, torch.ones(d, 1, device="cuda"), tdp.F32, tdp.DEVICE, d, 1)
+        for which in (tdp.E_LM_HEAD, tdp.E_LM_HEAD_I8):
+            tdp.tdp_ends_set_weight(e, which, w, tdp.BF16, tdp.DEVICE, d, vocab)
+            lg, tok, lp, tok2 = torch.empty(M, vocab, device="cuda"), i32([0] * M), torch.zeros(M, device="cuda"), i32([0] * M)
+            tdp.tdp_lm_head(e, x, M, None, M, lg, tok)
+            tdp.tdp_lm_head_logprobs(e, x, M, None, M, None, 0, tok2, lp, None, None, None)
+            ref = torch.log_softmax(lg, 1).max(1).values
+            assert torch.equal(tok.long(), lg.argmax(1)) and torch.equal(tok, tok2)
+            assert (lp - ref).abs().max().item() <= 1e-4      # (both in fp32)
+            del lg, ref
+    finally:
+        tdp.tdp_ends_destroy(e)
