@@ -398,7 +398,8 @@ typedef struct {
 #define TDP_E_LM_HEAD 2    /* [d_model, vocab_size] row-major ([in, out] like every projection) */
 #define TDP_E_LM_HEAD_I8 3 /* the same, held in 8-bit integers with a scale for each token of the vocabulary (see tdp_linear_i8); the
                               rows are then quantised behind the final norm.  d_model is at most 131072.  The projection is in the
-                              form that was set last. */
+                              form that was set last.  The bf16 matrix's memory is given back if none was set before and no call has
+                              read it (zeros); setting one takes it again. */
 TDP_API int tdp_ends_create(const tdp_ends_config* cfg, tdp_ends** out);
 TDP_API void tdp_ends_destroy(tdp_ends* e);
 /* src: host or device (mem), fp32 or bf16 (dtype).  Waits for the device's work on all streams first (a source may be written by any,

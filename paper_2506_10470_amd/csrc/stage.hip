@@ -788,8 +788,9 @@ struct tdp_ends {
   int64_t v_pad = 0;
   uint16_t* table = nullptr;   // bf16 [vocab][d]
   float* gain = nullptr;       // [d]
-  // the vocabulary projection: bf16 [v_pad][d] in layout_weights, or (int8) codes [v_pad][d_pad] with scales
-  uint16_t* w_head = nullptr;
+  // the vocabulary projection: bf16 [v_pad][d] in layout_weights (zeros at first), or (int8) codes [v_pad][d_pad] with scales
+  uint16_t* w_head = nullptr;  // null behind int8, where bf16 weights were neither set nor read before
+  bool bf16_used = false;      // a call has read w_head, or it was set: graphs may read it from now on
   bool int8 = false;
   int64_t d_pad = 0;           // d rounded up to the 128 codes of a k-tile
   uint8_t* head_codes = nullptr;
@@ -862,8 +863,7 @@ void tdp_ends_destroy(tdp_ends* e) {
   delete e;
 }
 
-// What a vocabulary projection in 8 bits needs, from the first time on that one is set.  (The bf16 matrix stays: a graph that was captured
-// before still reads it.)
+// What a vocabulary projection in 8 bits needs, from the first time on that one is set.
 static hipError_t int8_head_memory(tdp_ends* e) {
   const int64_t M = ((int64_t)e->cfg.max_tokens + 1) & ~1ll;
   hipError_t err = few_rows_setup();
@@ -918,6 +918,7 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   hipError_t err = hipSuccess;
   unsigned* column_max = nullptr;
   if (int8) err = int8_head_memory(e);
+  if (which == TDP_E_LM_HEAD && !e->w_head) err = dev_alloc(&e->w_head, e->v_pad * d, true);
   if (int8 && err == hipSuccess) err = dev_alloc(&column_max, V, false);
   if (err == hipSuccess) {
     if (which == TDP_E_EMBEDDING) err = launch_to_bf16(dsrc, f32, V * d, e->table, 0);
@@ -929,7 +930,14 @@ int tdp_ends_set_weight(tdp_ends* e, int32_t which, const void* src, int32_t dty
   if (err == hipSuccess) err = hipDeviceSynchronize();
   if (tmp) (void)hipFree(tmp);
   if (column_max) (void)hipFree(column_max);
-  if (head && err == hipSuccess) e->int8 = int8;
+  if (head && err == hipSuccess) {
+    e->int8 = int8;
+    e->bf16_used |= !int8;
+    if (!e->bf16_used && e->w_head) {  // (a matrix that was used stays: a graph that was captured before still reads it)
+      (void)hipFree(e->w_head);
+      e->w_head = nullptr;
+    }
+  }
   if (err != hipSuccess) return fail_hip(err, "weight conversion");
   return TDP_OK;
 }
@@ -986,6 +994,7 @@ static hipError_t project_rows(tdp_ends* e, const void* hidden_in, int32_t n_row
     g.A = e->y_codes; g.a_scale = e->y_scale; g.W = e->head_codes; g.w_scale = e->head_scale; g.Kpad = e->d_pad / 2;
   } else {
     g.A = e->y; g.W = e->w_head; g.Kpad = d;
+    e->bf16_used = true;
   }
   g.a_layout = layout_paired(g.Kpad); g.Npad = e->v_pad; g.M = M; g.N_store = V;
   g.out = logits; g.ldo = V; g.epilogue = EPI_STORE; g.out_f32 = 1;

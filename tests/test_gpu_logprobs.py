@@ -326,6 +326,55 @@ def test_an_8_bit_head_is_close_to_the_bf16_one_and_can_be_set_back():
         assert 1e-4 < ((a - b).norm() / a.norm()).item() < 0.03
 
 
+def test_an_8_bit_head_takes_less_memory_than_a_bf16_one():
+    """2048 x 65536 weights: 256 MiB in bf16, 128 in 8 bits.  What the object holds besides is the same but for codes of rows and scales."""
+    vocab, d, M = 65536, 2048, 8
+    w = torch.zeros(d, vocab, device="cuda", dtype=torch.bfloat16)
+    taken = {}
+    for which in (tdp.E_LM_HEAD, tdp.E_LM_HEAD_I8):
+        torch.cuda.synchronize()
+        before = torch.cuda.mem_get_info()[0]
+        e = tdp.tdp_ends_create(tdp.EndsConfig(vocab, d, 1e-5, M))
+        tdp.tdp_ends_set_weight(e, which, w, tdp.BF16, tdp.DEVICE, d, vocab)
+        taken[which] = (before - torch.cuda.mem_get_info()[0]) / 2 ** 20
+        tdp.tdp_ends_destroy(e)
+    assert taken[tdp.E_LM_HEAD] - taken[tdp.E_LM_HEAD_I8] >= 128 - 16, taken
+
+
+@pytest.mark.parametrize("first", ["nothing", "a call", "bf16 weights"])
+def test_the_forms_of_a_head_in_any_order(first):
+    """The bf16 matrix comes back where it was given back, and stays where a call or a captured one has read it."""
+    M, vocab, d = 20, 4100, 128
+    with Head(vocab, d, M, False) as bf16, Head(vocab, d, M, True) as int8:
+        x = bf16.rows(M, 1)
+        want, want8 = bf16.logits(x, M)[0], int8.logits(x, M)[0]
+    head = Head.__new__(Head)
+    head.vocab, head.d, head.weights = vocab, d, bf16.weights
+    head.h = tdp.tdp_ends_create(tdp.EndsConfig(vocab, d, 1e-5, M))
+    with head:
+        tdp.tdp_ends_set_weight(head.h, tdp.E_FINAL_NORM, bf16.gain, tdp.F32, tdp.DEVICE, d, 1)
+        graph = None
+        if first != "nothing":
+            if first == "bf16 weights":
+                head.set(False)
+            lg, captured = head.logits(x, M)[0], torch.zeros(M, vocab, device="cuda")
+            assert torch.equal(lg, want if first == "bf16 weights" else torch.zeros_like(lg))
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+                tdp.tdp_lm_head(head.h, x, M, None, M, captured, None, torch.cuda.current_stream())
+        for _ in range(2):
+            head.set(True)
+            assert torch.equal(head.logits(x, M)[0], want8)
+            if graph:                                   # the form that it was captured with
+                captured.fill_(7)
+                graph.replay()
+                torch.cuda.synchronize()
+                assert torch.equal(captured, lg)
+            head.set(False)
+            assert torch.equal(head.logits(x, M)[0], want)
+            lg = want
+
+
 @pytest.mark.parametrize("int8", [False, True])
 def test_rows_by_index_and_hidden_states_that_are_not_numbers(int8):
     M, vocab, d = 9, 4100, 128
