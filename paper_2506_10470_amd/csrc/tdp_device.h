@@ -188,8 +188,10 @@ __device__ __forceinline__ LogSum of_lane(const LogSum& l, int lane_xor) {
   return LogSum{__shfl_xor(l.max, lane_xor, 64), __shfl_xor(l.sum, lane_xor, 64), __shfl_xor(l.weighted, lane_xor, 64)};
 }
 
-// silu(z) = z / (1 + e^-z), with the hardware reciprocal (1 ulp) in place of an IEEE division: the
-// gated epilogue evaluates it 128 times per lane and tile, and its result is rounded to bf16 anyway.
+// silu(z) = z / (1 + e^-z), with the hardware's exponential and reciprocal (1 ulp): a gated epilogue evaluates it 128 times per lane
+// and tile.  e^-z is off by (|z| + 2) u, u = 2^-24, for z as it is; a z that three roundings have made of an integer sum and two
+// scales has already cost 3 |z| u, so that an exact exponential would take a gated result in fp32 from (4 |z| + 16) u to no less
+// than 3 |z| u.  Below z = -87 the reciprocal is subnormal and may be 0, and with it the result.
 __device__ __forceinline__ float silu_f(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 
 __device__ __forceinline__ float wave_sum(float v) {
