@@ -341,7 +341,8 @@ TDP_API int tdp_stage_timing_read(tdp_stage* st, float* ms /* host [8] */);
  * y = x W with both held as 8-bit integers, a scale for each row of x (token) and each column of W (output
  * channel), and exact sums: half the bytes of a bf16 projection to stream (what bounds a decode step's projections,
  * Sec. 3.4) and twice its matrix rate.  A vector v is held as codes c and a scale: with a = max |v| the scale is a / 127
- * and c = rint(v * (127 / a)), each operation rounded in fp32; an element is off by at most half a scale.
+ * and c = rint(v * (127 / a)), each operation rounded in fp32; an element is off by at most (1/2 + 2^-15) scales, and 2^-143 more
+ * where the scale is subnormal (a below 127 * 2^-126; a vector below 127 * 2^-150 has scale 0).
  *   y[m][n] = scale_x[m] * scale_w[n] * sum_k c_x[m][k] c_w[k][n]
  * The sum is a whole number, so a row's result does not depend on the other rows of the call.  A row or column that holds an
  * infinity or a NaN has scale NaN, and with it its whole result; one of zeros has scale 0.

@@ -1,9 +1,9 @@
 // The product in 8-bit integers with a scale for each token and each output channel (tdp_linear_i8_*): quantisation of rows and of
 // weights, and the object that holds the weights.  The product itself is the GEMM of gemm.hip on integers.
 //
-//   y[m, n] = s_x[m] s_w[n] sum_k c_x[m, k] c_w[k, n],    v = s c + e with |e| <= s / 2,  s = max |v| / 127
+//   y[m, n] = s_x[m] s_w[n] sum_k c_x[m, k] c_w[k, n],    v = s c + e with |e| <= s / 2 before rounding,  s = max |v| / 127
 //
-// The sum is exact, so all that is lost is lost in the codes; the scales are common to a sum and stand outside it.
+// (Rounded in fp32, c and s add 381 u s, u = 2^-24: v * (127 / a) is off by 2 u of up to 127, and s by u.)  The sum is exact, so all that is lost is lost in the codes; the scales are common to a sum and stand outside it.
 #include <math.h>
 #include <stdio.h>
 #include <string.h>

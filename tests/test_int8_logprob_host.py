@@ -25,6 +25,19 @@ def test_quantised_values_are_within_half_a_scale():
     assert (np.abs(codes * scales[:, None].astype(np.float64) - v) <= scales[:, None] * (0.5 + 1e-4)).all()
 
 
+def test_quantised_values_of_every_magnitude_are_within_the_stated_distance():
+    """(1/2 + 2^-15) scales, 381 roundings of 2^-24 beside the half; 2^-143 more, 127 codes of half of 2^-149, where the scale is subnormal."""
+    rng = np.random.default_rng(4)
+    with np.errstate(under="ignore"):
+        v = (rng.uniform(-1, 1, (3000, 40)) * 2.0 ** rng.uniform(-149, 127, (3000, 1))).astype(np.float32)
+    codes, scales = Q.quantise(v)
+    scales = scales.astype(np.float64)[:, None]
+    off = np.abs(codes * scales - v.astype(np.float64))
+    subnormal = scales < 2.0 ** -126
+    assert subnormal.any() and (scales == 0).any() and np.abs(codes).max() == 127
+    assert (off <= scales * (0.5 + 2.0 ** -15) + np.where(subnormal, 2.0 ** -143, 0)).all()
+
+
 def test_product_by_hand():
     y = Q.product(np.array([[1, 2], [3, -4]]), [0.5, 2], np.array([[10, 20], [-1, 0], [0, 1]]), [1, 4, 0.25])
     assert y.tolist() == [[25, -2, 0.25], [-100, -24, -2]]
