@@ -648,7 +648,12 @@ int tdp_gemm_plan_i8(int32_t M, int32_t N, int32_t K, int32_t gated, int64_t wor
   if (workspace_elems < 0) return fail(TDP_EINVAL, "negative workspace");
   if (!plan) return fail(TDP_EINVAL, "null pointer");
   const int64_t Npad = gated ? 2 * round_up(N / 2, 128) : round_up(N, 256);
-  const GemmPlan p = gemm_plan({M, 0, 0, gated ? EPI_SWIGLU : EPI_STORE, false, true, Npad, round_up(K, 128) / 2, workspace_elems});
+  GemmPlan p;
+  try {
+    p = gemm_plan({M, 0, 0, gated ? EPI_SWIGLU : EPI_STORE, false, true, Npad, round_up(K, 128) / 2, workspace_elems});
+  } catch (...) {  // (the plan is remembered)
+    return fail(TDP_ENOMEM, "host allocation failed");
+  }
   plan[0] = p.tile;
   gemm_tile_size(p.tile, plan + 1, plan + 2);
   plan[3] = p.splits;
