@@ -156,10 +156,10 @@ struct Share {
 // on their way meanwhile.  A wave takes four weight rows, in 1 KiB loads of four rows x four k-blocks of 64 codes, eight of them at a
 // time, and a lane multiplies its 16 codes with those of every row by v_dot4_i32_i8; the lanes of a weight row are added up at the end.
 // Where there are too few weight rows for the chip the waves of a workgroup share K (slices). Taken where one round of workgroups holds
-// all weight rows (up to 16384 columns): one row of 256 x 256 3.4 us (tiles 5.8), 4096 x 4096 6.3 (11.1), 5120 x 7168 9.8 (13.4), 8192 x
-// 8192 13.9 (17.8), 28672 x 8192 43 (44: 5.4 TB/s); two rows 4.2, 8.3, 11.5, 15.2, 44.  With more weight rows the tiles' longer runs of
-// memory win: 4096 x 32000 26.0 (24.4), 8192 x 57344 in several turns 93 (72).  With four rows a workgroup's own quantisation costs what
-// is saved (4096 x 4096 12 and 11).
+// all weight rows (up to 16384 columns).  Calls of a captured graph, back to back: one row of 256 x 256 3.5 us (tiles 5.9), 4096 x 4096 6.2
+// (11.6), 5120 x 7168 9.5 (14.3), 8192 x 8192 14.1 (19.3), 28672 x 8192 43 (44: 5.4 TB/s); two rows 4.3, 8.2, 11.3, 15.6, 44.  (By itself
+// the smallest takes 4 to 5 in a trace.)  With more weight rows the tiles' longer runs of memory win: 4096 x 32000 26.0 (24.4), 8192 x
+// 57344 in several turns 93 (72).  With four rows a workgroup's own quantisation costs what is saved (4096 x 4096 12 and 11).
 constexpr int kFewRows = 2, kFewWaves = 8, kFewInFlight = 8, kFewLds = 128 * 1024;
 struct FewRowsParams : FewRowsArgs {
   int slices, groups, blocks_k;  // waves that share K; groups of four weight rows; k-blocks
