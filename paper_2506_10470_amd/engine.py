@@ -25,10 +25,13 @@ class OutOfPages(RuntimeError):
 
 
 def _on_own_stream(method):
-    """The method with the worker's stream as the current one: torch's copies are then ordered with the kernels, and memory that it
-    takes and gives back is reused behind them."""
+    """The method with the worker's stream as the current one, behind what the caller's current stream holds: torch's copies are then
+    ordered with the kernels, and memory that it takes and gives back is reused behind them."""
     @functools.wraps(method)
     def run(self, *args):
+        callers = torch.cuda.current_stream()
+        if callers != self.torch_stream:
+            self.torch_stream.wait_stream(callers)
         with torch.cuda.stream(self.torch_stream):
             return method(self, *args)
     return run
@@ -45,8 +48,8 @@ class StageWorker:
     def __init__(self, tdp, stage: int, ends: int, d_model: int, num_pages: int, max_pages_per_seq: int,
                  max_batch: int, max_tokens: int, max_seqs: int, prompts: Sequence[Sequence[int]], stream=None,
                  check_tables: bool = False, logprobs: Optional[int] = None):
-        """stream: a torch stream or its address (none: the current one); all of the worker's work is ordered on it, and what
-        the caller has queued elsewhere for these handles is the caller's to wait for.  logprobs: the log-probability of every
+        """stream: a torch stream or its address (none: the current one); all of the worker's work is ordered on it, behind
+        what the caller's current stream holds at each event.  logprobs: the log-probability of every
         generated token goes to self.logprobs[i] (beside self.generated[i]), and of the `logprobs` likeliest tokens in its place
         (0: none) as (token, log-probability) pairs to self.top[i].  check_tables: validate every call's block tables on the GPU
         first (tdp_stage_check_*): one synchronisation per call, for runs that test the allocator rather than the throughput."""

@@ -25,8 +25,11 @@ def streams(monkeypatch):
         def __init__(self, name):
             self.name = name
 
+        def wait_stream(self, other):
+            State.waits.append((self.name, other.name, len(State.copies)))
+
     class State:
-        kind, current, copies = Stream, Stream("caller's"), []
+        kind, current, copies, waits = Stream, Stream("caller's"), [], []
 
     @contextlib.contextmanager
     def stream(s):
@@ -66,3 +69,7 @@ def test_copies_and_buffers_are_on_the_stream_of_the_calls(streams, own, logprob
     assert [len(g) for g in w.generated] == [2, 2] and streams.current.name == "another"
     assert tdp.calls and all(s is mine for _, s in tdp.calls)
     assert len(streams.copies) >= 8 and set(streams.copies) == {mine.name}
+    # each event is behind what the caller's stream holds: prefill and decode wait in front of their first copy
+    events = [(a, b) for a, b, _ in streams.waits]
+    assert events == [(mine.name, "caller's")] * own + [(mine.name, "another")] * 2
+    assert all(at < len(streams.copies) for _, _, at in streams.waits) and len({at for _, _, at in streams.waits}) == len(events)
