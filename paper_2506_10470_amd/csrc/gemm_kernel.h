@@ -44,7 +44,8 @@ struct GemmStatsParams : GemmParams {
 // Operands of 8-bit integers: 64 codes where 32 bf16 stood, byte for byte the same tiles, rings and fragments (offsets and strides count
 // pairs of codes), v_mfma_i32_16x16x64_i8 in the place of v_mfma_f32_16x16x32_bf16 - the same cycles for twice the products.  The
 // accumulators are int32 in the registers of the fp32 ones, and so are the partials of a split: a sum over K is exact (a lane's
-// |sum| <= 127 * 128 K - weights may hold -128 - which K <= 2^17 keeps below 2^31), so a result does not depend on the plan or on the batch around it.
+// |sum| <= 127 * 128 K - weights may hold -128 - which K <= 2^17 keeps below 2^31), so a result does not depend on the plan or on the
+// batch around it.
 struct GemmIntParams : GemmParams {
   static constexpr bool kIntegers = true;
   const float* a_scale;  // [M]

@@ -3,7 +3,8 @@
 //
 //   y[m, n] = s_x[m] s_w[n] sum_k c_x[m, k] c_w[k, n],    v = s c + e with |e| <= s / 2 before rounding,  s = max |v| / 127
 //
-// (Rounded in fp32, c and s add 381 u s, u = 2^-24: v * (127 / a) is off by 2 u of up to 127, and s by u.)  The sum is exact, so all that is lost is lost in the codes; the scales are common to a sum and stand outside it.
+// (Rounded in fp32, c and s add 381 u s, u = 2^-24: v * (127 / a) is off by 2 u of up to 127, and s by u.)  The sum is exact, so all that
+// is lost is lost in the codes; the scales are common to a sum and stand outside it.
 #include <math.h>
 #include <stdio.h>
 #include <string.h>

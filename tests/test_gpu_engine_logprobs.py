@@ -81,7 +81,7 @@ def test_the_worker_refuses_more_alternatives_than_there_can_be():
 
 
 def run_on(stream, sh, reqs, prompts, busy):
-    """A schedule with log-probabilities on `stream` (None: the current one), behind `busy` milliseconds or so of other work on it."""
+    """A schedule with log-probabilities on `stream` (None: the current one), each event behind `busy` passes over 1 GiB on it."""
     capacity, budget = 600, 128
     max_len = max(r[0] + r[1] for r in reqs) + 1
     max_pps = (max_len + 15) // 16 + 1
