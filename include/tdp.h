@@ -446,6 +446,52 @@ TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_r
                                  const int32_t* targets, int32_t n_top, int32_t* next_token, float* logprob, float* entropy,
                                  int32_t* top_index, float* top_logprob, void* stream);
 
+/* ---- several continuations of a prompt -------------------------------------------------------------
+ * What a batch needs whose rows continue one another's tokens: block tables that fork and pages that are copied when they do.  All of it works
+ * on device memory and only enqueues. */
+
+/* Block tables that fork.  A row is a length, lens[r] tokens, and the ceil(lens[r] / 16) first entries of its table row: the pages that hold
+ * them.  refs[p] counts the table entries that name page p, and whoever else holds it (prompts kept for later, other batches); a page with
+ * refs 0 is free.  tdp_pages_fork makes n_dst new rows from n_src old ones:
+ *   - row r continues row parents[r] (-1: a new, empty row) with room for add[r] more tokens (add null: add_all for every row), so
+ *     dst_lens[r] = src_lens[parents[r]] + add[r].  parents null: row r continues row r, rows from n_src on are new
+ *   - full pages are shared.  A last page that is partly filled can be written by one row only: the first (lowest) row that continues its
+ *     row takes it over, if it is named nowhere else (refs 1); every other one gets a fresh page in its place, and copies[r] = (that page, the
+ *     fresh one), to be given to tdp_stage_kv_copy_pages of every stage that holds these pages; copies[r] = (-1, -1) otherwise
+ *   - old rows that nothing continues are released, and with them the pages that nothing names any more
+ * Fresh pages are those with refs_in 0, lowest ids first, dealt to the rows in order and within a row to its entries in order; pages
+ * released by a call are free from the next one on, so no page is read and written by the copies of one call.
+ * refs_out may be refs_in itself.  status (dev int32 [4]): pages that are missing, rows that are refused (a parent or length out of range, a
+ * last page outside the pool), fresh pages taken, pages that were free.  If a page is missing or a row refused nothing happens: refs_out is
+ * refs_in, copies are (-1, -1), dst_tables and dst_lens are left as they are.  Entries of dst_tables behind a row's pages are -1.
+ * n_src = 0 makes new rows alone, n_dst = 0 releases all.  Page ids in src_tables are trusted as everywhere; reference counts of ids
+ * outside the pool are skipped.
+ *   parents, add, dst_lens dev int32 [n_dst]; copies dev int32 [n_dst][2]; src_lens dev int32 [n_src]; src_tables, dst_tables
+ *   dev int32 [n_src], [n_dst] [max_pages_per_seq], not overlapping; refs_in, refs_out dev int32 [num_pages] */
+typedef struct tdp_pages tdp_pages;
+typedef struct {
+  int32_t num_pages;          /* 1 .. 2^22 */
+  int32_t max_rows;           /* rows on either side, 1 .. 8192 */
+  int32_t max_pages_per_seq;  /* width of a block-table row, up to 2^16 */
+} tdp_pages_config;
+TDP_API int tdp_pages_create(const tdp_pages_config* cfg, tdp_pages** out);
+TDP_API void tdp_pages_destroy(tdp_pages* h); /* owns scratch alone; as a tdp_linear_i8 for devices, streams and graphs */
+TDP_API int tdp_pages_fork(tdp_pages* h, const int32_t* parents, const int32_t* src_tables, const int32_t* src_lens, int32_t n_src,
+                           const int32_t* add, int32_t add_all, int32_t n_dst, const int32_t* refs_in, int32_t* refs_out,
+                           int32_t* dst_tables, int32_t* dst_lens, int32_t* copies, int32_t* status, void* stream);
+/* Pages in use moved towards the front of the pool, at most max_moves of them: the k-th move takes the k-th highest movable page to the k-th
+ * lowest free one, as long as that is lower.  Movable are pages that the n_rows given rows name and nobody else holds (refs equal to
+ * the entries that name them); others stay.  dst_tables (may be src_tables itself) are the rows with the new ids, -1 behind a row's pages,
+ * moves (dev int32 [max_moves][2]) the (old, new) ids for tdp_stage_kv_copy_pages, (-1, -1) behind the last.  status: 0, rows that are
+ * refused (a length out of range, an id outside the pool; nothing moves then), moves, pages in use.  max_moves 1 .. num_pages. */
+TDP_API int tdp_pages_compact(tdp_pages* h, const int32_t* src_tables, const int32_t* lens, int32_t n_rows, int32_t max_moves,
+                              const int32_t* refs_in, int32_t* refs_out, int32_t* dst_tables, int32_t* moves, int32_t* status,
+                              void* stream);
+/* Keys and values of whole pages copied within the stage, in all its layers: page pairs[i][0] to page pairs[i][1], i < n (dev int32
+ * [n][2]).  Pairs with an id outside [0, num_pages) are skipped.  The pairs are independent: no page is the target of two, nor the target
+ * of one and the source of another. */
+TDP_API int tdp_stage_kv_copy_pages(tdp_stage* st, const int32_t* pairs, int32_t n, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -78,6 +78,7 @@ struct tdp_stage {
   int maxM = 0;
   int layer_first = 0, layer_count = 0;  // count 0 = all layers
   int decode_span = 0;                   // 0 = chosen from the batch size
+  int device = 0;
   bool timing = false;
   std::vector<hipEvent_t> ev_start, ev_stop;
   std::vector<int> ev_class;
@@ -319,6 +320,7 @@ int tdp_stage_create(const tdp_stage_config* cfg, tdp_stage** out) {
   tdp_stage* st = new (std::nothrow) tdp_stage();
   if (!st) return fail(TDP_ENOMEM, "host allocation failed");
   st->cfg = *cfg;
+  (void)hipGetDevice(&st->device);
   const tdp_stage_config& c = st->cfg;
   const int64_t d = c.d_model, dh = c.head_dim, L = c.n_layers;
   st->dq = (int64_t)c.n_q_heads * dh;
@@ -541,6 +543,23 @@ int tdp_stage_kv_export(tdp_stage* st, int32_t layer, void* k_packed, void* v_pa
                         int32_t total_tokens, void* stream) {
   return kv_copy_common(0, st, layer, k_packed, v_packed, cu_seqlens, block_tables, n_seqs, total_tokens,
                         stream);
+}
+
+static int check_stage_device(const tdp_stage* st) {
+  int dev = -1;
+  HIP_TRY(hipGetDevice(&dev));
+  return dev == st->device ? TDP_OK : fail(TDP_EINVAL, "the stage was created on another device than the current one");
+}
+
+int tdp_stage_kv_copy_pages(tdp_stage* st, const int32_t* pairs, int32_t n, void* stream) {
+  if (!st) return fail(TDP_EINVAL, "null stage");
+  if (n < 0) return fail(TDP_EINVAL, "negative size");
+  if (n == 0) return TDP_OK;
+  if (!pairs) return fail(TDP_EINVAL, "null pointer");
+  const int rc = check_stage_device(st);
+  if (rc != TDP_OK) return rc;
+  HIP_TRY(launch_kv_copy_pages(kv_layout(st, 0), st->pool_bytes, st->cfg.n_layers, pairs, n, (hipStream_t)stream));
+  return TDP_OK;
 }
 
 int tdp_stage_prefill(tdp_stage* st, const void* hidden_in, const int32_t* cu_seqlens,

@@ -250,6 +250,10 @@ hipError_t launch_kv_copy(int to_pages, void* k_packed, void* v_packed, const Kv
                           const int32_t* cu_seqlens, int n_seqs, int total_tokens,
                           const int32_t* block_tables, int max_pages_per_seq, hipStream_t s);
 
+// Whole pages copied within the pools of n_layers layers, layer_bytes apart (kv: those of the first): pairs dev [n][2], (from, to); pairs with an
+// id outside the pool are skipped.
+hipError_t launch_kv_copy_pages(const KvLayout& kv, int64_t layer_bytes, int n_layers, const int32_t* pairs, int n, hipStream_t s);
+
 // Validation of the tables of a decode (lens = ctx_lens[n_rows]) or prefill (lens = cu_seqlens[n_rows + 1])
 // call.  owner: scratch int32[num_pages]; res: int32[2] = {violations, min(row * 8 + kind)} with kind
 // 1 = length, 2 = page id, 3 = written page shared, 4 = cu_seqlens ends.  Reads the tables in bounds on any input.

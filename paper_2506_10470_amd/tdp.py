@@ -45,6 +45,10 @@ E_EMBEDDING, E_FINAL_NORM, E_LM_HEAD, E_LM_HEAD_I8 = 0, 1, 2, 3
 MAX_TOP = 32
 
 
+class PagesConfig(C.Structure):
+    _fields_ = [("num_pages", C.c_int32), ("max_rows", C.c_int32), ("max_pages_per_seq", C.c_int32)]
+
+
 class TdpError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__("tdp error %d: %s" % (code, msg))
@@ -102,6 +106,11 @@ _SIGS = {
     "tdp_linear_i8_set_bias": (C.c_int, [_vp, _vp, _i32, _i32, _i64]),
     "tdp_linear_i8_set_form": (C.c_int, [_vp, _i32, _i32]),
     "tdp_linear_i8_run": (C.c_int, [_vp, _vp, _i32, _i64, _i32, _vp, _i64, _vp, _i32, _i64, _vp]),
+    "tdp_pages_create": (C.c_int, [C.POINTER(PagesConfig), C.POINTER(_vp)]),
+    "tdp_pages_destroy": (None, [_vp]),
+    "tdp_pages_fork": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "tdp_pages_compact": (C.c_int, [_vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "tdp_stage_kv_copy_pages": (C.c_int, [_vp, _vp, _i32, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(lib, _name)
@@ -332,3 +341,28 @@ def tdp_linear_i8_set_form(h, tile: int, splits: int = 1) -> None:
 def tdp_linear_i8_run(h, x, x_dtype, ld_x, M, residual, ld_residual, out, out_dtype, ld_out, stream=None) -> None:
     _check(lib.tdp_linear_i8_run(h, _ptr(x), x_dtype, ld_x, M, _ptr(residual), ld_residual, _ptr(out), out_dtype, ld_out,
                                  _stream(stream)))
+
+
+def tdp_pages_create(cfg: PagesConfig) -> int:
+    h = _vp()
+    _check(lib.tdp_pages_create(C.byref(cfg), C.byref(h)))
+    return h.value
+
+
+def tdp_pages_destroy(h) -> None:
+    lib.tdp_pages_destroy(h)
+
+
+def tdp_pages_fork(h, parents, src_tables, src_lens, n_src, add, add_all, n_dst, refs_in, refs_out, dst_tables, dst_lens, copies, status,
+                   stream=None) -> None:
+    _check(lib.tdp_pages_fork(h, _ptr(parents), _ptr(src_tables), _ptr(src_lens), n_src, _ptr(add), add_all, n_dst, _ptr(refs_in),
+                              _ptr(refs_out), _ptr(dst_tables), _ptr(dst_lens), _ptr(copies), _ptr(status), _stream(stream)))
+
+
+def tdp_pages_compact(h, src_tables, lens, n_rows, max_moves, refs_in, refs_out, dst_tables, moves, status, stream=None) -> None:
+    _check(lib.tdp_pages_compact(h, _ptr(src_tables), _ptr(lens), n_rows, max_moves, _ptr(refs_in), _ptr(refs_out), _ptr(dst_tables),
+                                 _ptr(moves), _ptr(status), _stream(stream)))
+
+
+def tdp_stage_kv_copy_pages(st, pairs, n, stream=None) -> None:
+    _check(lib.tdp_stage_kv_copy_pages(st, _ptr(pairs), n, _stream(stream)))
