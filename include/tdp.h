@@ -447,8 +447,38 @@ TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_r
                                  int32_t* top_index, float* top_logprob, void* stream);
 
 /* ---- several continuations of a prompt -------------------------------------------------------------
- * What a batch needs whose rows continue one another's tokens: block tables that fork and pages that are copied when they do.  All of it works
- * on device memory and only enqueues. */
+ * What a batch needs whose rows continue one another's tokens: the choice of the likeliest continuations over beams and vocabulary, and
+ * block tables that fork, with pages that are copied when they do.  All of it works on device memory and only enqueues. */
+
+/* Beam selection.  The rows of logits are beams, `beams` of them to a group (a request).  Beam b of a group, with the score s_b it has so
+ * far, can be continued by every token t at
+ *   c(b, t) = s_b + z_b[t] - ln sum_j exp z_b[j];      a finished beam by end_token alone, at s_b.
+ * For every group the n_out best continuations are given in order, of equal ones the lower beam first, then the larger logit, then the lower
+ * token:
+ *   parent[g][j]    row of logits that it continues (group * beams + beam)
+ *   token[g][j], score[g][j]
+ *   finished_out[g][j]   1 if the token is end_token, else 0 (may be null)
+ * A continuation of minus infinity or NaN is none (a beam whose score is minus infinity, a masked token, and a row with a NaN, with plus
+ * infinity or with nothing but minus infinity, which has no distribution); places behind the last have parent and token -1, score minus
+ * infinity, finished_out 0.  The candidates are compared in 64 bits: a row's sum of exponentials is formed in fp32 per thread (64 terms at
+ * most) and joined in 64.
+ *   logits   dev, TDP_F32 or TDP_BF16, [n_groups * beams][n], rows ld >= n elements apart, at any alignment of their type
+ *   scores   dev fp32 [n_groups * beams]
+ *   finished dev int32 [n_groups * beams], not 0: finished; or null.  end_token: in [0, n), or, with finished null, -1: none
+ * beams 1 .. TDP_MAX_BEAMS, n_out 1 .. TDP_MAX_TOP and at most beams * n, n up to 2^27, n_groups * beams <= max_rows (0: nothing to do).
+ * A tdp_beams owns scratch.  It lives on the device that is current when it is created, calls on it need that device current, and it must
+ * not be driven from two streams at once, nor by two captured graphs that replay at once. */
+#define TDP_MAX_BEAMS 32
+typedef struct tdp_beams tdp_beams;
+typedef struct {
+  int32_t max_rows; /* rows of logits per call, 1 .. 2^16 */
+  int32_t max_out;  /* n_out, 1 .. TDP_MAX_TOP */
+} tdp_beams_config;
+TDP_API int tdp_beams_create(const tdp_beams_config* cfg, tdp_beams** out);
+TDP_API void tdp_beams_destroy(tdp_beams* h);
+TDP_API int tdp_beams_select(tdp_beams* h, const void* logits, int32_t dtype, int32_t n_groups, int32_t beams, int32_t n, int64_t ld,
+                             const float* scores, const int32_t* finished, int32_t end_token, int32_t n_out, int32_t* parent,
+                             int32_t* token, float* score, int32_t* finished_out, void* stream);
 
 /* Block tables that fork.  A row is a length, lens[r] tokens, and the ceil(lens[r] / 16) first entries of its table row: the pages that hold
  * them.  refs[p] counts the table entries that name page p, and whoever else holds it (prompts kept for later, other batches); a page with
@@ -475,7 +505,7 @@ typedef struct {
   int32_t max_pages_per_seq;  /* width of a block-table row, up to 2^16 */
 } tdp_pages_config;
 TDP_API int tdp_pages_create(const tdp_pages_config* cfg, tdp_pages** out);
-TDP_API void tdp_pages_destroy(tdp_pages* h); /* owns scratch alone; as a tdp_linear_i8 for devices, streams and graphs */
+TDP_API void tdp_pages_destroy(tdp_pages* h); /* owns scratch alone; a device, streams and graphs as a tdp_beams */
 TDP_API int tdp_pages_fork(tdp_pages* h, const int32_t* parents, const int32_t* src_tables, const int32_t* src_lens, int32_t n_src,
                            const int32_t* add, int32_t add_all, int32_t n_dst, const int32_t* refs_in, int32_t* refs_out,
                            int32_t* dst_tables, int32_t* dst_lens, int32_t* copies, int32_t* status, void* stream);
@@ -483,7 +513,7 @@ TDP_API int tdp_pages_fork(tdp_pages* h, const int32_t* parents, const int32_t* 
  * lowest free one, as long as that is lower.  Movable are pages that the n_rows given rows name and nobody else holds (refs equal to
  * the entries that name them); others stay.  dst_tables (may be src_tables itself) are the rows with the new ids, -1 behind a row's pages,
  * moves (dev int32 [max_moves][2]) the (old, new) ids for tdp_stage_kv_copy_pages, (-1, -1) behind the last.  status: 0, rows that are
- * refused (a length out of range, an id outside the pool; nothing moves then), moves, pages in use.  max_moves 1 .. num_pages. */
+ * refused (a length out of range, an id outside the pool; nothing moves then), moves, pages in use.  max_moves 1 .. 2^22. */
 TDP_API int tdp_pages_compact(tdp_pages* h, const int32_t* src_tables, const int32_t* lens, int32_t n_rows, int32_t max_moves,
                               const int32_t* refs_in, int32_t* refs_out, int32_t* dst_tables, int32_t* moves, int32_t* status,
                               void* stream);

@@ -1,0 +1,395 @@
+// The n_out best continuations of every group of beams, from rows of logits: score of the beam + ln softmax of its row.
+//
+// Two launches.  The first reads the logits once: a workgroup has a piece of a row (a whole row where there are many), notes its largest logit,
+// the sum of exponentials relative to that, and its n_out largest logits in order.  Within a row, candidates are in the order of
+// the logits, so nothing else of the row can be chosen.  The second has a workgroup to a group: it joins the sums of every row and ranks the
+// candidates of all beams.
+//
+// Scores of different beams are often close, and which token goes on depends on their order, so what is compared is in 64 bits.  The
+// exponentials are in fp32: e^d as 2^(d log2 e), the product in two parts, so that all of it but the instruction's own error (1 ulp, in no
+// order) and the sums of a thread's terms is exact to 2^-24 of a term.  Over thousands of terms that averages out to below 1e-8 of the sum.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdio.h>
+
+#include <algorithm>
+#include <new>
+#include <type_traits>
+
+#include "../../include/tdp.h"
+#include "logit_rows.h"
+#include "tdp_device.h"
+#include "tdp_kernels.h"
+
+namespace tdp {
+
+int probe_fail(int code, const char* msg);  // sets the thread's error message (stage.hip)
+
+namespace {
+
+typedef unsigned long long u64;
+constexpr int kInFlight = 8;    // vectors of a thread
+constexpr int kListsMost = 1024;  // of a group
+constexpr int kPiecesMost = 64, kPiecesOfMany = 8;
+constexpr int kIndexBits = 27;  // of a token, beside 5 of a beam and 32 of a logit's order
+static_assert(TDP_MAX_BEAMS <= 32 && TDP_MAX_BEAMS * kPiecesOfMany <= kListsMost && TDP_MAX_TOP <= kTopMost, "what the second kernel holds");
+
+struct BeamArgs {
+  int beams, n, width, pieces, k;  // width: columns of a piece
+  const int32_t* finished;
+  int end_token;
+  const float* scores;
+  // per (row, piece)
+  float* max;
+  double* sum;
+  u64* keys;  // [k], in order, 0 behind the last
+  int32_t *parent, *token;
+  float* score;
+  int32_t* finished_out;
+};
+
+// e^d for d <= 0
+__device__ __forceinline__ float exp_close(float d) {
+  constexpr float kHigh = 1.44269502f, kLow = 1.92596299e-8f;  // log2 e
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(d, kHigh, fmaxf(d, -1e30f) * kLow));
+}
+
+// A piece of a row in vectors from its first element on, wherever that lies in memory: which terms a thread adds up, and with them
+// the bits of the sum, do not depend on it, so that beams that are alike are equal.  What is left behind the last whole vector is the first
+// threads', an element each.
+typedef u32x4 __attribute__((aligned(4))) u32x4_of_float;
+typedef u32x4 __attribute__((aligned(2))) u32x4_of_bf16;
+template <typename T>
+struct BeamRow {
+  static constexpr int kPer = 16 / sizeof(T);
+  typedef typename std::conditional<sizeof(T) == 4, u32x4_of_float, u32x4_of_bf16>::type Anywhere;
+  const T* first;
+  int n, body;
+  __device__ __forceinline__ BeamRow(const T* row, int n_) : first(row), n(n_), body(n_ / kPer) {}
+  __device__ __forceinline__ int index(int v, int e) const { return v * kPer + e; }
+  __device__ __forceinline__ u32x4 load(int v) const { return *reinterpret_cast<const Anywhere*>(first + (int64_t)v * kPer); }
+  __device__ __forceinline__ float at(int i) const { return (float)first[i]; }
+  __device__ __forceinline__ int edge(int tid) const { return body * kPer + tid < n ? body * kPer + tid : -1; }
+};
+
+__device__ __forceinline__ double wave_sum_double(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// KEEP: a thread has eight vectors at most and keeps them in registers; else the piece is read twice, and the tokens of threads whose
+// largest logit is among the wanted a third time.
+template <typename T, bool KEEP>
+__global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restrict__ logits, int64_t ld, int shift, const BeamArgs a) {
+  __shared__ RowShared rs;
+  __shared__ TopShared ts;
+  __shared__ double wave_total[16];
+  extern __shared__ __attribute__((aligned(16))) unsigned char staged_raw[];  // (KEEP) StagedUnits of every wave
+  StagedUnits& staged = reinterpret_cast<StagedUnits*>(staged_raw)[threadIdx.x >> 6];
+  const int tid = threadIdx.x, threads = blockDim.x, wave = tid >> 6, lane = tid & 63, waves = threads >> 6;
+  const int slot = blockIdx.x, m = slot / a.pieces, piece = slot - m * a.pieces;
+  u64* const keys = a.keys + (int64_t)slot * a.k;
+  if (a.finished && a.finished[m]) {  // the end token alone, at no cost
+    for (int i = tid; i < a.k; i += threads) keys[i] = piece == 0 && i == 0 ? key_of(0.f, a.end_token) : 0;
+    if (tid == 0) {
+      a.max[slot] = piece == 0 ? 0.f : -INFINITY;
+      a.sum[slot] = piece == 0 ? 1.0 : 0.0;
+    }
+    return;
+  }
+  typedef LogitRow<T> Values;
+  typedef BeamRow<T> Row;
+  constexpr int kPer = Row::kPer;
+  const int first = piece * a.width;
+  const Row row(logits + (int64_t)m * ld + first, min(a.width, a.n - first));
+  u32x4 z[kInFlight];
+  auto fetch = [&](int v0) {
+#pragma unroll
+    for (int u = 0; u < kInFlight; ++u) z[u] = v0 + u * threads < row.body ? row.load(v0 + u * threads) : Values::nothing();
+  };
+  float own_max = -INFINITY;
+  auto take_max = [&] {
+#pragma unroll
+    for (int u = 0; u < kInFlight; ++u)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) own_max = fmaxf(own_max, Values::value(z[u], e));
+  };
+  const int edge_at = row.edge(tid);
+  if constexpr (KEEP) fetch(tid);
+  const float edge = edge_at >= 0 ? row.at(edge_at) : -INFINITY;
+  if constexpr (KEEP) {
+    take_max();
+  } else {
+#pragma unroll 1
+    for (int v0 = tid; v0 < row.body; v0 += threads * kInFlight) {
+      fetch(v0);
+      take_max();
+    }
+  }
+  // the maximum of all, and on the way those of 64 groups of lanes
+  float v = fmaxf(own_max, edge);
+  auto group = [&](int size) {
+    if (waves == size && (lane & (size - 1)) == size - 1) rs.group_max[wave * (64 / size) + lane / size] = v;
+  };
+  group(1);
+  v = fmaxf(v, from_front<kDppShift1, 0xf>(v, v));
+  group(2);
+  v = fmaxf(v, from_front<kDppShift2, 0xf>(v, v));
+  group(4);
+  v = fmaxf(v, from_front<kDppShift4, 0xf>(v, v));
+  group(8);
+  v = fmaxf(v, from_front<kDppShift8, 0xf>(v, v));
+  group(16);
+  v = fmaxf(v, from_front<kDppLast15, 0xa>(v, v));
+  v = fmaxf(v, from_front<kDppLast31, 0xc>(v, v));
+  if (lane == 63) rs.wave_max[wave] = v;
+  if (tid == 0) ts.listed = 0;
+  __syncthreads();
+  float max = rs.wave_max[0];
+  for (int w = 1; w < waves; ++w) max = fmaxf(max, rs.wave_max[w]);
+  // sums relative to it: a few terms in fp32, the rest in 64 bits
+  const float r = reference_of(max);
+  double total = edge_at >= 0 ? (double)exp_close(edge - r) : 0.0;
+  auto add = [&](int v0) {
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < kInFlight; ++u) {
+      if (u > 0 && v0 - tid + u * threads >= row.body) break;  // (the same for all threads)
+      asm volatile("" : "+v"(z[u]));  // (bf16: converted here again, the values of two passes would not fit)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) sum += exp_close(Values::value(z[u], e) - r);
+    }
+    total += (double)sum;
+  };
+  if constexpr (KEEP) {
+    add(tid);
+  } else {
+#pragma unroll 1
+    for (int v0 = tid; v0 < row.body; v0 += threads * kInFlight) {
+      fetch(v0);
+      add(v0);
+    }
+  }
+  total = wave_sum_double(total);
+  if (lane == 0) wave_total[wave] = total;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < waves; ++w) total += wave_total[w];
+    a.max[slot] = max;
+    a.sum[slot] = total;
+  }
+  const int found = select_top(
+      rs, ts, row, max, min(a.k, row.n), edge, edge_at, 1, shift, [&](int) { return own_max; },
+      [&](int, int at) {
+        ts.units[wave][at] = tid;
+        if constexpr (KEEP) {
+#pragma unroll
+          for (int u = 0; u < kInFlight; ++u) staged[at][u] = z[u];
+        }
+      },
+      [&](int at_slot, int j, int& at) {
+        const int vec = ts.units[wave][at_slot] + j / kPer * threads;
+        if (vec >= row.body) return 0.f;
+        at = row.index(vec, j % kPer);
+        if constexpr (KEEP) {
+          const unsigned* const p = reinterpret_cast<const unsigned*>(staged[at_slot]);
+          if constexpr (sizeof(T) == 4) return __uint_as_float(p[j]);
+          else return __uint_as_float(j & 1 ? p[j / 2] & 0xffff0000u : p[j / 2] << 16);
+        } else {
+          return row.at(at);
+        }
+      },
+      [&](int place, int index, float value) { keys[place] = key_of(value, first + index); });
+  for (int i = found + tid; i < a.k; i += threads) keys[i] = 0;
+}
+
+// A candidate's place among all of its group as two whole numbers, the larger the better: its score, 0 for none, and what decides
+// between equal ones.
+struct Candidate {
+  u64 score, rest;
+};
+__device__ __forceinline__ bool better(const Candidate& x, const Candidate& y) {
+  return x.score > y.score || (x.score == y.score && x.rest > y.rest);
+}
+__device__ __forceinline__ double score_of(u64 order) {
+  return __longlong_as_double((long long)(order ^ (order >> 63 ? 1ull << 63 : ~0ull)));
+}
+
+// One workgroup per group.  `lists` = beams * pieces lists of k candidates, each in order.  The first `heads` of every list, n_out in all or
+// more, give a bound: the n_out-th best of them.  A list goes on behind its heads only if all of them reach the bound, so at
+// most n_out / heads lists do, and n_out * k / heads <= 1024 candidates reach it: one to a thread, a few dozen as a rule.
+__global__ __launch_bounds__(1024) void beams_group_kernel(const BeamArgs a) {
+  __shared__ double log_total[TDP_MAX_BEAMS];
+  __shared__ Candidate pool[kListsMost];
+  __shared__ Candidate bound;
+  __shared__ int count;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = blockIdx.x;
+  const int64_t slot0 = (int64_t)g * a.beams * a.pieces;
+  for (int b = wave; b < a.beams; b += 16) {
+    const bool in = lane < a.pieces;
+    const int64_t slot = slot0 + b * a.pieces + lane;
+    const float own = in ? a.max[slot] : -INFINITY;
+    float max = own;
+    for (int o = 1; o < 64; o *= 2) max = fmaxf(max, __shfl_xor(max, o, 64));
+    const double part = in ? a.sum[slot] * exp((double)own - (double)max) : 0.0;  // (nothing but minus infinity: NaN)
+    const double total = wave_sum_double(part);
+    if (lane == 0) log_total[b] = (double)max + log(total);
+  }
+  if (tid == 0) {
+    bound = Candidate{0, 0};
+    count = 0;
+  }
+  __syncthreads();
+  const int lists = a.beams * a.pieces, heads = (a.k + lists - 1) / lists, some = lists * heads;
+  auto candidate = [&](int list, int pos) {
+    const u64 key = a.keys[(slot0 + list) * a.k + pos];
+    if (!key) return Candidate{0, 0};
+    const int beam = list / a.pieces;
+    const unsigned order = (unsigned)(key >> 32);
+    const double c = (double)a.scores[(int64_t)g * a.beams + beam] + ((double)logit_of(order) - log_total[beam]);
+    if (!(c > -INFINITY)) return Candidate{0, 0};
+    const long long bits = __double_as_longlong(c + 0.0);
+    return Candidate{(u64)bits ^ (bits < 0 ? ~0ull : 1ull << 63),
+                     (u64)(31 - beam) << 59 | (u64)order << kIndexBits | ((unsigned)key & ((1u << kIndexBits) - 1))};
+  };
+  auto rank = [&](const Candidate& c, int n) {
+    int r = 0;
+    for (int i = 0; i < n; ++i) r += better(pool[i], c);
+    return r;
+  };
+  Candidate own{0, 0};
+  if (tid < some) pool[tid] = own = candidate(tid / heads, tid % heads);
+  __syncthreads();
+  if (own.score && rank(own, some) == a.k - 1) bound = own;  // (no two are equal)
+  __syncthreads();
+  const Candidate least = bound;
+  for (int i = tid; i < lists * a.k; i += 1024) {
+    const Candidate c = candidate(i / a.k, i % a.k);
+    if (c.score && !better(least, c)) pool[atomicAdd(&count, 1)] = c;
+  }
+  __syncthreads();
+  const int n = count, n_out = a.k;
+  if (tid < n) {
+    own = pool[tid];
+    const int place = rank(own, n);
+    if (place < n_out) {
+      const int64_t at = (int64_t)g * n_out + place;
+      const int token = (int)(~own.rest & ((1u << kIndexBits) - 1));
+      a.parent[at] = g * a.beams + 31 - (int)(own.rest >> 59);
+      a.token[at] = token;
+      a.score[at] = (float)score_of(own.score);
+      if (a.finished_out) a.finished_out[at] = token == a.end_token;
+    }
+  }
+  for (int i = n + tid; i < n_out; i += 1024) {
+    const int64_t at = (int64_t)g * n_out + i;
+    a.parent[at] = a.token[at] = -1;
+    a.score[at] = -INFINITY;
+    if (a.finished_out) a.finished_out[at] = 0;
+  }
+}
+
+int fail_hip(hipError_t e, const char* what) {
+  char buf[200];
+  snprintf(buf, sizeof buf, "%s: %s", what, hipGetErrorString(e));
+  return probe_fail(e == hipErrorOutOfMemory ? TDP_ENOMEM : TDP_EHIP, buf);
+}
+
+// Pieces of a row.  Enough of them that a few rows keep the chip busy, no smaller than a few KiB; a row of many in pieces that the
+// registers of a workgroup hold, as long as they are not too many.
+int pieces_of(int rows, int n, int per) {
+  const int full = (n + per * kInFlight * 1024 - 1) / (per * kInFlight * 1024);
+  const int wanted = std::min({kPiecesMost, kListsMost / 2 / rows, n / (per * 1024)});
+  return std::max(1, std::max(std::min(full, kPiecesOfMany), wanted));
+}
+
+}  // namespace
+}  // namespace tdp
+
+using namespace tdp;
+
+struct tdp_beams {
+  tdp_beams_config cfg;
+  int device = 0;
+  float* max = nullptr;
+  double* sum = nullptr;
+  u64* keys = nullptr;
+};
+
+extern "C" {
+
+int tdp_beams_create(const tdp_beams_config* cfg, tdp_beams** out) {
+  if (!cfg || !out) return probe_fail(TDP_EINVAL, "null pointer");
+  if (cfg->max_rows < 1 || cfg->max_rows > (1 << 16)) return probe_fail(TDP_EINVAL, "max_rows must be 1 .. 2^16");
+  if (cfg->max_out < 1 || cfg->max_out > TDP_MAX_TOP) return probe_fail(TDP_EINVAL, "max_out must be 1 .. TDP_MAX_TOP");
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return probe_fail(TDP_EHIP, "no HIP device");
+  tdp_beams* h = new (std::nothrow) tdp_beams();
+  if (!h) return probe_fail(TDP_ENOMEM, "host allocation failed");
+  h->cfg = *cfg;
+  h->device = dev;
+  const size_t slots = std::max<size_t>(kListsMost, (size_t)kPiecesOfMany * cfg->max_rows);
+  hipError_t e = hipMalloc((void**)&h->max, slots * sizeof(float));
+  if (e == hipSuccess) e = hipMalloc((void**)&h->sum, slots * sizeof(double));
+  if (e == hipSuccess) e = hipMalloc((void**)&h->keys, slots * cfg->max_out * sizeof(u64));
+  if (e != hipSuccess) {
+    const int code = fail_hip(e, "tdp_beams_create");
+    tdp_beams_destroy(h);
+    return code;
+  }
+  *out = h;
+  return TDP_OK;
+}
+
+void tdp_beams_destroy(tdp_beams* h) {
+  if (!h) return;
+  (void)hipDeviceSynchronize();
+  void* ptrs[] = {h->max, h->sum, h->keys};
+  for (void* p : ptrs)
+    if (p) (void)hipFree(p);
+  delete h;
+}
+
+int tdp_beams_select(tdp_beams* h, const void* logits, int32_t dtype, int32_t n_groups, int32_t beams, int32_t n, int64_t ld,
+                     const float* scores, const int32_t* finished, int32_t end_token, int32_t n_out, int32_t* parent, int32_t* token,
+                     float* score, int32_t* finished_out, void* stream) {
+  if (!h) return probe_fail(TDP_EINVAL, "null beams object");
+  if (dtype != TDP_F32 && dtype != TDP_BF16) return probe_fail(TDP_EINVAL, "dtype must be TDP_F32 or TDP_BF16");
+  if (n_groups < 0 || n < 1 || n > (1 << kIndexBits) || ld < n) return probe_fail(TDP_EINVAL, "bad shape");
+  if (beams < 1 || beams > TDP_MAX_BEAMS) return probe_fail(TDP_EINVAL, "beams must be 1 .. TDP_MAX_BEAMS");
+  if (n_out < 1 || n_out > h->cfg.max_out || n_out > (int64_t)beams * n) return probe_fail(TDP_EINVAL, "n_out must be 1 .. max_out and at most beams * n");
+  if ((int64_t)n_groups * beams > h->cfg.max_rows) return probe_fail(TDP_EINVAL, "rows exceed max_rows");
+  if (end_token >= n || end_token < (finished ? 0 : -1)) return probe_fail(TDP_EINVAL, "end_token must be a token, or -1 where no beam can be finished");
+  if (n_groups == 0) return TDP_OK;
+  if (!logits || !scores || !parent || !token || !score) return probe_fail(TDP_EINVAL, "null pointer");
+  if ((uintptr_t)logits & (dtype == TDP_F32 ? 3 : 1)) return probe_fail(TDP_EINVAL, "logits must be aligned to their type");
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return fail_hip(e, "hipGetDevice");
+  if (dev != h->device) return probe_fail(TDP_EINVAL, "the object was created on another device than the current one");
+  hipStream_t s = (hipStream_t)stream;
+  const int rows = n_groups * beams, per = dtype == TDP_F32 ? 4 : 8, pieces = pieces_of(rows, n, per);
+  const int width = ((n + pieces - 1) / pieces + 7) / 8 * 8, used = (n + width - 1) / width, vectors = (std::min(width, n) + per - 1) / per;
+  int threads = 64;  // two vectors to a thread, if 1024 are enough for that
+  while (threads < 1024 && threads * 2 < vectors) threads *= 2;
+  const bool keep = vectors <= threads * kInFlight;
+  int shift = 0;  // of the elements that a thread has read
+  while ((1 << shift) < (vectors + threads - 1) / threads * per) ++shift;
+  const BeamArgs a{beams, n, width, used, n_out, finished, end_token, scores, h->max, h->sum, h->keys, parent, token, score, finished_out};
+  const unsigned grid = (unsigned)rows * used;
+  const size_t lds = keep ? threads / 64 * sizeof(StagedUnits) : 0;
+#define TDP_PIECES(T, KEEP) beams_piece_kernel<T, KEEP><<<grid, threads, lds, s>>>((const T*)logits, ld, shift, a)
+  if (dtype == TDP_F32) {
+    if (keep) TDP_PIECES(float, true); else TDP_PIECES(float, false);
+  } else {
+    if (keep) TDP_PIECES(bf16, true); else TDP_PIECES(bf16, false);
+  }
+#undef TDP_PIECES
+  beams_group_kernel<<<n_groups, 1024, 0, s>>>(a);
+  e = hipGetLastError();
+  return e == hipSuccess ? TDP_OK : fail_hip(e, "tdp_beams_select");
+}
+
+}  // extern "C"

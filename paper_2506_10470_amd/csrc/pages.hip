@@ -505,7 +505,7 @@ int tdp_pages_compact(tdp_pages* h, const int32_t* src_tables, const int32_t* le
   if (!h) return probe_fail(TDP_EINVAL, "null pages object");
   if (n_rows < 0) return probe_fail(TDP_EINVAL, "negative size");
   if (n_rows > h->cfg.max_rows) return probe_fail(TDP_EINVAL, "rows exceed max_rows");
-  if (max_moves < 1 || max_moves > h->cfg.num_pages) return probe_fail(TDP_EINVAL, "max_moves must be 1 .. num_pages");
+  if (max_moves < 1 || max_moves > kChunk * kChunksMost) return probe_fail(TDP_EINVAL, "max_moves must be 1 .. 2^22");
   if (!refs_in || !refs_out || !moves || !status) return probe_fail(TDP_EINVAL, "null pointer");
   if (n_rows > 0 && (!src_tables || !lens || !dst_tables)) return probe_fail(TDP_EINVAL, "null pointer");
   const int64_t bytes = 4ll * h->cfg.max_pages_per_seq * n_rows, N = h->cfg.num_pages;

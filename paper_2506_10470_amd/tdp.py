@@ -43,6 +43,11 @@ class LinearI8Config(C.Structure):
 
 E_EMBEDDING, E_FINAL_NORM, E_LM_HEAD, E_LM_HEAD_I8 = 0, 1, 2, 3
 MAX_TOP = 32
+MAX_BEAMS = 32
+
+
+class BeamsConfig(C.Structure):
+    _fields_ = [("max_rows", C.c_int32), ("max_out", C.c_int32)]
 
 
 class PagesConfig(C.Structure):
@@ -106,6 +111,9 @@ _SIGS = {
     "tdp_linear_i8_set_bias": (C.c_int, [_vp, _vp, _i32, _i32, _i64]),
     "tdp_linear_i8_set_form": (C.c_int, [_vp, _i32, _i32]),
     "tdp_linear_i8_run": (C.c_int, [_vp, _vp, _i32, _i64, _i32, _vp, _i64, _vp, _i32, _i64, _vp]),
+    "tdp_beams_create": (C.c_int, [C.POINTER(BeamsConfig), C.POINTER(_vp)]),
+    "tdp_beams_destroy": (None, [_vp]),
+    "tdp_beams_select": (C.c_int, [_vp, _vp, _i32, _i32, _i32, _i32, _i64, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
     "tdp_pages_create": (C.c_int, [C.POINTER(PagesConfig), C.POINTER(_vp)]),
     "tdp_pages_destroy": (None, [_vp]),
     "tdp_pages_fork": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -341,6 +349,22 @@ def tdp_linear_i8_set_form(h, tile: int, splits: int = 1) -> None:
 def tdp_linear_i8_run(h, x, x_dtype, ld_x, M, residual, ld_residual, out, out_dtype, ld_out, stream=None) -> None:
     _check(lib.tdp_linear_i8_run(h, _ptr(x), x_dtype, ld_x, M, _ptr(residual), ld_residual, _ptr(out), out_dtype, ld_out,
                                  _stream(stream)))
+
+
+def tdp_beams_create(cfg: BeamsConfig) -> int:
+    h = _vp()
+    _check(lib.tdp_beams_create(C.byref(cfg), C.byref(h)))
+    return h.value
+
+
+def tdp_beams_destroy(h) -> None:
+    lib.tdp_beams_destroy(h)
+
+
+def tdp_beams_select(h, logits, dtype, n_groups, beams, n, ld, scores, finished, end_token, n_out, parent, token, score,
+                     finished_out=None, stream=None) -> None:
+    _check(lib.tdp_beams_select(h, _ptr(logits), dtype, n_groups, beams, n, ld, _ptr(scores), _ptr(finished), end_token, n_out,
+                                _ptr(parent), _ptr(token), _ptr(score), _ptr(finished_out), _stream(stream)))
 
 
 def tdp_pages_create(cfg: PagesConfig) -> int:
