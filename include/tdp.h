@@ -447,8 +447,9 @@ TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_r
                                  int32_t* top_index, float* top_logprob, void* stream);
 
 /* ---- several continuations of a prompt -------------------------------------------------------------
- * What a batch needs whose rows continue one another's tokens: the choice of the likeliest continuations over beams and vocabulary, and
- * block tables that fork, with pages that are copied when they do.  All of it works on device memory and only enqueues. */
+ * What a batch needs whose rows continue one another's tokens: the choice of the likeliest continuations over beams and vocabulary,
+ * block tables that fork and pages that are copied when they do, and attention that reads a prefix which several rows share
+ * once.  All of it works on device memory and only enqueues, so that a step (attention, head, choice, tables, copies) needs no host. */
 
 /* Beam selection.  The rows of logits are beams, `beams` of them to a group (a request).  Beam b of a group, with the score s_b it has so
  * far, can be continued by every token t at
@@ -521,6 +522,23 @@ TDP_API int tdp_pages_compact(tdp_pages* h, const int32_t* src_tables, const int
  * [n][2]).  Pairs with an id outside [0, num_pages) are skipped.  The pairs are independent: no page is the target of two, nor the target
  * of one and the source of another. */
 TDP_API int tdp_stage_kv_copy_pages(tdp_stage* st, const int32_t* pairs, int32_t n, void* stream);
+
+/* Attention of rows that share prefixes.  Rows group_starts[g] .. group_starts[g + 1] - 1 of the batch (dev int32 [n_groups + 1], from 0 to batch,
+ * ascending; a group may be empty) are a group: rows whose block tables may begin with the same pages, such as the beams of a prompt or requests
+ * behind one system prompt.  The leading whole pages in which the tables of all rows of a group agree, in front of every row's last
+ * token, are found in the tables and read once for the group; so results are those of attention row by row, within rounding, whatever
+ * the groups are.  n_groups = 0 (group_starts null): every row for itself.  n_groups <= max_batch.
+ * tdp_stage_decode_shared is tdp_stage_decode with groups (one batch, whatever decode_micro_batches says).
+ * tdp_stage_attend is the attention alone, on one layer's pools: row b attends to the lens[b] tokens that its pages hold,
+ *   out[b][h] = sum_t softmax_t(q[b][h] . k[t][h / group] / sqrt(head_dim)) v[t][h / group],
+ * zeros where lens[b] is 0 (or less; a length beyond 16 * max_pages_per_seq counts as that).  q dev bf16 [batch][n_q_heads][head_dim], rotated as
+ * the keys are, 16-byte aligned; out the same, 8-byte aligned, not overlapping q; lens dev int32 [batch].  It writes no page.
+ * Scores, softmax statistics and sums are fp32; probabilities are rounded to bf16 for the product with the values.  Both calls use the stage's
+ * scratch, so they are ordered with its other calls, and need its device current. */
+TDP_API int tdp_stage_attend(tdp_stage* st, int32_t layer, const void* q, const int32_t* lens, const int32_t* block_tables, int32_t batch,
+                             const int32_t* group_starts, int32_t n_groups, void* out, void* stream);
+TDP_API int tdp_stage_decode_shared(tdp_stage* st, const void* hidden_in, const int32_t* ctx_lens, const int32_t* block_tables, int32_t batch,
+                                    const int32_t* group_starts, int32_t n_groups, void* hidden_out, void* stream);
 
 #ifdef __cplusplus
 }

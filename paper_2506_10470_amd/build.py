@@ -17,7 +17,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtdp.so")
 SCHED_LIB = os.path.join(HERE, "libtdp_sched.so")
 SOURCES = ("gemm.hip", "gemm_int.hip", "gemm_stats.hip", "attention.hip", "elementwise.hip", "stage.hip", "probe.hip",
-           "gemm_static.hip", "linear_i8.hip", "logprob.hip", "pages.hip", "beams.hip")
+           "gemm_static.hip", "linear_i8.hip", "logprob.hip", "pages.hip", "beams.hip",
+           "attention_shared.hip")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]

@@ -65,6 +65,7 @@ struct tdp_stage {
     unsigned* spans_done = nullptr;  // finished spans of every (request, K/V head): zero between launches
     int4* attn_items = nullptr;     // decode work list, rebuilt every step
     int32_t* attn_item_pages = nullptr;  // physical pages of every item's span
+    SharedScratch shared = {};      // (the first set) what rows of a group share
   };
   Scratch sc[2];
   int n_scratch = 1;
@@ -165,10 +166,42 @@ KvLayout kv_layout(tdp_stage* st, int layer) {
   return kv;
 }
 
-// The layer sequence shared by both phases.  M tokens; decode when ctx_lens != null.
+// Rows of a decode batch in groups that may share a prefix.
+struct Groups {
+  const int32_t* starts;
+  int n;
+};
+
+// Plan and kernels of attention over groups, in the first scratch set; rows attend to lens + add tokens.
+hipError_t plan_shared(tdp_stage* st, const Groups& groups, const int32_t* lens, int add, const int32_t* block_tables, int batch, int span_len,
+                       hipStream_t s) {
+  const tdp_stage_config& c = st->cfg;
+  tdp_stage::Scratch& sc = st->sc[0];
+  if (groups.n > 0) {
+    const hipError_t e = launch_attn_shared_plan(groups.starts, groups.n, lens, add, block_tables, c.max_pages_per_seq, batch, c.n_q_heads,
+                                                 c.n_kv_heads, sc.shared, s);
+    if (e != hipSuccess) return e;
+  }
+  const SharedRows rows{groups.n > 0 ? sc.shared.row_pages : nullptr, sc.shared.span_pages, add};
+  return launch_attn_plan(lens, block_tables, c.max_pages_per_seq, batch, st->max_chunks, span_len, sc.attn_items, sc.attn_item_pages, s, &rows);
+}
+hipError_t attend_shared(tdp_stage* st, const Groups& groups, const void* q, int64_t ld, const KvLayout& kv, const int32_t* block_tables, int batch,
+                         int span_len, void* out, const OperandLayout& out_layout, hipStream_t s) {
+  const tdp_stage_config& c = st->cfg;
+  tdp_stage::Scratch& sc = st->sc[0];
+  if (groups.n > 0) {
+    const hipError_t e = launch_attn_prefix(q, ld, batch, groups.n, c.n_q_heads, kv, sc.shared, block_tables, c.max_pages_per_seq, sc.part_o, sc.part_ml,
+                                            st->max_chunks, s);
+    if (e != hipSuccess) return e;
+  }
+  return launch_attn_decode(DecodeQueries{q, ld, nullptr, nullptr, nullptr, 1}, batch, c.n_q_heads, kv, sc.attn_items, sc.attn_item_pages, span_len / 16,
+                            nullptr, sc.part_o, sc.part_ml, sc.spans_done, st->max_chunks, span_len, out, out_layout, s, true);
+}
+
+// The layer sequence shared by both phases.  M tokens; decode when ctx_lens != null, with groups if some are given.
 int run_layers(tdp_stage* st, tdp_stage::Scratch& sc, bool timed, const void* hidden_in, void* hidden_out, int M,
                const int32_t* ctx_lens, const int32_t* cu_seqlens, int n_seqs, const int32_t* block_tables,
-               hipStream_t s) {
+               hipStream_t s, const Groups* groups = nullptr) {
   const tdp_stage_config& c = st->cfg;
   const int64_t d = c.d_model;
   if (timed) st->ev_used = 0;
@@ -178,11 +211,12 @@ int run_layers(tdp_stage* st, tdp_stage::Scratch& sc, bool timed, const void* hi
   const void* x = hidden_in;
   int x_f32 = 0;
   const int span_len = st->decode_span > 0 ? st->decode_span : attn_decode_span(M, c.n_kv_heads);
-  const bool planned = ctx_lens && attn_decode_planned(M, c.n_kv_heads, st->max_chunks, span_len);
+  const bool planned = ctx_lens && !groups && attn_decode_planned(M, c.n_kv_heads, st->max_chunks, span_len);
+  if (groups) HIP_TRY(plan_shared(st, *groups, ctx_lens, 1, block_tables, M, span_len, s));
   if (planned)
     HIP_TRY(launch_attn_plan(ctx_lens, block_tables, c.max_pages_per_seq, M, st->max_chunks, span_len, sc.attn_items,
                              sc.attn_item_pages, s));
-  const bool count_spans = attn_decode_counts_spans(M, c.n_q_heads, c.n_kv_heads, st->max_chunks, span_len);
+  const bool count_spans = groups || attn_decode_counts_spans(M, c.n_q_heads, c.n_kv_heads, st->max_chunks, span_len);
   const int l_begin = st->layer_count > 0 ? st->layer_first : 0;
   const int l_end = st->layer_count > 0 ? st->layer_first + st->layer_count : c.n_layers;
   // A projection whose K range was split leaves fp32 partials in the workspace; the kernel that
@@ -232,7 +266,7 @@ int run_layers(tdp_stage* st, tdp_stage::Scratch& sc, bool timed, const void* hi
     }
     // a3: rotary embedding + KV append, from the fp32 projection (if it was split: sums the partials and adds the bias, which the
     // GEMM's epilogue has done otherwise); in small decode batches inside the attention kernel
-    const bool split = qkv_splits > 1, rotates = ctx_lens && attn_decode_rotates(M, c.n_kv_heads, st->max_chunks, span_len);
+    const bool split = qkv_splits > 1, rotates = ctx_lens && !groups && attn_decode_rotates(M, c.n_kv_heads, st->max_chunks, span_len);
     const DecodeQueries dq{rotates ? nullptr : sc.qkv, st->Nqkv_pad, split ? sc.ws : sc.qkv32, split ? g.bias : nullptr, st->rope_table,
                            qkv_splits};
     if (rotated) {
@@ -247,7 +281,9 @@ int run_layers(tdp_stage* st, tdp_stage::Scratch& sc, bool timed, const void* hi
     g.bias = nullptr;
     {  // a4: attention
       Timer t(st, s, timed, T_ATTN);
-      if (ctx_lens)
+      if (groups)
+        HIP_TRY(attend_shared(st, *groups, sc.qkv, st->Nqkv_pad, kv, block_tables, M, span_len, sc.attn, layout_paired(st->dq), s));
+      else if (ctx_lens)
         HIP_TRY(launch_attn_decode(dq, M, c.n_q_heads, kv, planned ? sc.attn_items : nullptr,
                                    planned ? sc.attn_item_pages : block_tables,
                                    planned ? span_len / 16 : c.max_pages_per_seq, ctx_lens,
@@ -379,7 +415,14 @@ int tdp_stage_create(const tdp_stage_config* cfg, tdp_stage** out) {
     A(&sc.part_ml, mb * c.n_q_heads * st->max_chunks * 2, false);
     A(&sc.spans_done, mb * c.n_kv_heads, true);
     A(&sc.attn_items, mb * st->max_chunks, false);
-    if (i == 0) A(&sc.token_pages, c.max_tokens, false);
+    if (i == 0) {
+      A(&sc.token_pages, c.max_tokens, false);
+      A(&sc.shared.row_pages, mb, true);
+      A(&sc.shared.group_pages, mb, true);
+      A(&sc.shared.group_first, mb, true);
+      A(&sc.shared.span_pages, 1, true);
+      A(&sc.shared.items, 2 * (int64_t)attn_prefix_items_most(c.max_batch, c.n_q_heads, c.n_kv_heads), false);
+    }
     // spans longer than the minimum round the span count up: up to (1024 / 256 - 1) extra minimum spans' worth
     A(&sc.attn_item_pages, mb * (st->max_chunks + kDecodeSpanMax / kDecodeSpanMin) * (kDecodeSpanMin / 16), false);
   }
@@ -421,7 +464,8 @@ void tdp_stage_destroy(tdp_stage* st) {
     if (p) (void)hipFree(p);
   for (tdp_stage::Scratch& sc : st->sc) {
     void* sp[] = {sc.y, sc.qkv, sc.qkv32, sc.attn, sc.h, sc.u, sc.xa, sc.xb, sc.ws, sc.part_o, sc.part_ml,
-                  sc.spans_done, sc.attn_items, sc.attn_item_pages, sc.token_pages};
+                  sc.spans_done, sc.attn_items, sc.attn_item_pages, sc.token_pages, sc.shared.row_pages, sc.shared.group_pages,
+                  sc.shared.group_first, sc.shared.span_pages, sc.shared.items};
     for (void* p : sp)
       if (p) (void)hipFree(p);
   }
@@ -601,6 +645,44 @@ int tdp_stage_decode(tdp_stage* st, const void* hidden_in, const int32_t* ctx_le
   if (rc != TDP_OK) return rc;
   HIP_TRY(hipEventRecord(st->ev_join, st->aux_stream));
   HIP_TRY(hipStreamWaitEvent(s, st->ev_join, 0));
+  return TDP_OK;
+}
+
+static int check_groups(const tdp_stage* st, const int32_t* group_starts, int32_t n_groups) {
+  if (n_groups < 0 || n_groups > st->cfg.max_batch) return fail(TDP_EINVAL, "n_groups must be 0 .. max_batch");
+  if (n_groups > 0 && !group_starts) return fail(TDP_EINVAL, "null pointer");
+  return check_stage_device(st);
+}
+
+int tdp_stage_decode_shared(tdp_stage* st, const void* hidden_in, const int32_t* ctx_lens, const int32_t* block_tables, int32_t batch,
+                            const int32_t* group_starts, int32_t n_groups, void* hidden_out, void* stream) {
+  if (!st) return fail(TDP_EINVAL, "null stage");
+  if (batch < 0) return fail(TDP_EINVAL, "negative batch");
+  if (batch > st->cfg.max_batch) return fail(TDP_EINVAL, "batch exceeds max_batch");
+  if (batch == 0) return TDP_OK;
+  if (!hidden_in || !hidden_out || !ctx_lens || !block_tables) return fail(TDP_EINVAL, "null pointer");
+  const int rc = check_groups(st, group_starts, n_groups);
+  if (rc != TDP_OK) return rc;
+  const Groups groups{group_starts, n_groups};
+  return run_layers(st, st->sc[0], true, hidden_in, hidden_out, batch, ctx_lens, nullptr, batch, block_tables, (hipStream_t)stream, &groups);
+}
+
+int tdp_stage_attend(tdp_stage* st, int32_t layer, const void* q, const int32_t* lens, const int32_t* block_tables, int32_t batch,
+                     const int32_t* group_starts, int32_t n_groups, void* out, void* stream) {
+  if (!st) return fail(TDP_EINVAL, "null stage");
+  if (layer < 0 || layer >= st->cfg.n_layers) return fail(TDP_EINVAL, "layer out of range");
+  if (batch < 0) return fail(TDP_EINVAL, "negative batch");
+  if (batch > st->cfg.max_batch) return fail(TDP_EINVAL, "batch exceeds max_batch");
+  if (batch == 0) return TDP_OK;
+  if (!q || !out || !lens || !block_tables) return fail(TDP_EINVAL, "null pointer");
+  if (((uintptr_t)q & 15) || ((uintptr_t)out & 7)) return fail(TDP_EINVAL, "q must be 16-byte and out 8-byte aligned");
+  const int rc = check_groups(st, group_starts, n_groups);
+  if (rc != TDP_OK) return rc;
+  const Groups groups{group_starts, n_groups};
+  const int span_len = st->decode_span > 0 ? st->decode_span : attn_decode_span(batch, st->cfg.n_kv_heads);
+  hipStream_t s = (hipStream_t)stream;
+  HIP_TRY(plan_shared(st, groups, lens, 0, block_tables, batch, span_len, s));
+  HIP_TRY(attend_shared(st, groups, q, st->dq, kv_layout(st, layer), block_tables, batch, span_len, out, layout_row_major(st->dq), s));
   return TDP_OK;
 }
 

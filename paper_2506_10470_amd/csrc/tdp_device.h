@@ -67,6 +67,11 @@ __device__ __forceinline__ int decode_position(int ctx, int max_pages_per_seq) {
   return min(max(ctx, 0), max_pages_per_seq * 16 - 1);
 }
 
+// Softmax in the exp2 domain: a finite stand-in for -inf (exp2 gives exactly 0, no inf - inf), and by how much (log2 units) a block may
+// exceed the reference before sums are rescaled.
+constexpr float kNegBig = -1.0e30f;
+constexpr float kRescaleSlack = 8.0f;
+
 // Offset of element (r, k) in an operand laid out as
 // (r >> shift)*group + (k>>5)*kb + (r & (2^shift - 1))*par + (k&31).
 template <typename L>

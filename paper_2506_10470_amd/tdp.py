@@ -111,6 +111,8 @@ _SIGS = {
     "tdp_linear_i8_set_bias": (C.c_int, [_vp, _vp, _i32, _i32, _i64]),
     "tdp_linear_i8_set_form": (C.c_int, [_vp, _i32, _i32]),
     "tdp_linear_i8_run": (C.c_int, [_vp, _vp, _i32, _i64, _i32, _vp, _i64, _vp, _i32, _i64, _vp]),
+    "tdp_stage_attend": (C.c_int, [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp]),
+    "tdp_stage_decode_shared": (C.c_int, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp]),
     "tdp_beams_create": (C.c_int, [C.POINTER(BeamsConfig), C.POINTER(_vp)]),
     "tdp_beams_destroy": (None, [_vp]),
     "tdp_beams_select": (C.c_int, [_vp, _vp, _i32, _i32, _i32, _i32, _i64, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
@@ -390,3 +392,13 @@ def tdp_pages_compact(h, src_tables, lens, n_rows, max_moves, refs_in, refs_out,
 
 def tdp_stage_kv_copy_pages(st, pairs, n, stream=None) -> None:
     _check(lib.tdp_stage_kv_copy_pages(st, _ptr(pairs), n, _stream(stream)))
+
+
+def tdp_stage_attend(st, layer, q, lens, block_tables, batch, group_starts, n_groups, out, stream=None) -> None:
+    _check(lib.tdp_stage_attend(st, layer, _ptr(q), _ptr(lens), _ptr(block_tables), batch, _ptr(group_starts), n_groups, _ptr(out),
+                                _stream(stream)))
+
+
+def tdp_stage_decode_shared(st, hidden_in, ctx_lens, block_tables, batch, group_starts, n_groups, hidden_out, stream=None) -> None:
+    _check(lib.tdp_stage_decode_shared(st, _ptr(hidden_in), _ptr(ctx_lens), _ptr(block_tables), batch, _ptr(group_starts), n_groups,
+                                       _ptr(hidden_out), _stream(stream)))
