@@ -123,9 +123,10 @@ class Handle:
 
 
 class Memory:
-    """Device memory of the library, for torch.as_tensor."""
+    """Device memory of a library's object, for torch.as_tensor, whose tensors keep this and so the object alive."""
 
-    def __init__(self, address, count, kind):
+    def __init__(self, owner, address, count, kind):
+        self.owner = owner
         self.__cuda_array_interface__ = {"shape": (count,), "typestr": kind, "data": (address, False), "version": 2}
 
 
@@ -298,7 +299,7 @@ def prepare_own(S, case):
     for layer in range(layers):  # the stage's pools instead of the plain ones
         k, v, size = tdp.tdp_stage_kv_pool(stage, layer)
         for views, address, plain in ((ks, k, S.k), (vs, v, S.v)):
-            view = torch.as_tensor(Memory(address, size, "|u1"), device="cuda")
+            view = torch.as_tensor(Memory(S.owner, address, size, "|u1"), device="cuda")
             view = (view if S.kv8 else view.view(torch.bfloat16)).view(plain[layer].shape)
             view.copy_(plain[layer])
             views.append(view)
