@@ -16,15 +16,6 @@
 
 namespace tdp {
 
-// Floats past the caches of an XCD, for workgroups of other XCDs in the same launch.
-__device__ __forceinline__ void store_agent(float* p, float v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_agent2(const float* p) {  // (8-byte aligned)
-  return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED,
-                                                      __HIP_MEMORY_SCOPE_AGENT));
-}
-
 // =====================================================================================
 // Decode.  Work item = (request, span of span_len tokens of its context); one workgroup
 // of four waves per (item, kv head).  The four waves split the span's 32-token blocks evenly and
@@ -53,13 +44,10 @@ __device__ __forceinline__ float2 load_agent2(const float* p) {  // (8-byte alig
 // A length that its block-table row cannot hold is brought into the row's range (decode_position, also in the rotation), so
 // that the list never outgrows its buffer and the grid: every span counted here is made, and spans_done ends at zero,
 // whatever ctx_lens holds.
-// SHARED: what is planned is what a row has behind the pages that its group shares; an item then holds the tokens and pages from there on,
-// and in its last number how many spans of the prefix are in front of it.
-template <bool SHARED>
 __global__ __launch_bounds__(256) void attn_plan_kernel(const int32_t* __restrict__ ctx_lens, int batch, int span_len,
                                                         const int32_t* __restrict__ block_tables,
                                                         int max_pages_per_seq, int4* __restrict__ items, int max_items,
-                                                        int32_t* __restrict__ item_pages, const SharedRows shared) {
+                                                        int32_t* __restrict__ item_pages) {
   constexpr int NP = 16;      // parts of a span
   constexpr int NB = NP + 1;  // class 0: full spans; 1..NP: last span with > (NP-c)/NP of span_len
   __shared__ __attribute__((aligned(16))) int part[NB][256];  // counts of (class, thread); then how many items of the class lie in front
@@ -67,12 +55,6 @@ __global__ __launch_bounds__(256) void attn_plan_kernel(const int32_t* __restric
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (batch + 255) / 256;
   const int piece = span_len / NP;
-  auto prefix_of = [&](int b) { return SHARED ? shared.prefix(b, ctx_lens[b], max_pages_per_seq) : 0; };  // pages
-  auto tokens_of = [&](int b) {
-    if constexpr (SHARED) return shared.tokens(ctx_lens[b], max_pages_per_seq) - prefix_of(b) * 16;
-    else return decode_position(ctx_lens[b], max_pages_per_seq) + 1;
-  };
-  auto spans_of = [&](int n_total) { return SHARED ? max(1, (n_total + span_len - 1) / span_len) : (n_total + span_len - 1) / span_len; };
   auto last_class = [&](int n_total, int n) {  // tokens in the last span: 1 .. span_len
     const int rem = n_total - (n - 1) * span_len;
     return NP - min((rem - 1) / piece, NP - 1);
@@ -80,8 +62,8 @@ __global__ __launch_bounds__(256) void attn_plan_kernel(const int32_t* __restric
 #pragma unroll
   for (int c = 0; c < NB; ++c) part[c][tid] = 0;
   for (int b = tid * per; b < min((tid + 1) * per, batch); ++b) {
-    const int n_total = tokens_of(b);
-    const int n = spans_of(n_total);
+    const int n_total = decode_position(ctx_lens[b], max_pages_per_seq) + 1;
+    const int n = (n_total + span_len - 1) / span_len;
     part[0][tid] += n - 1;
     part[last_class(n_total, n)][tid] += 1;
   }
@@ -111,26 +93,26 @@ __global__ __launch_bounds__(256) void attn_plan_kernel(const int32_t* __restric
   const int b = blockIdx.x * 4 + wave;  // this wave's request
   if (b >= batch) return;
   const int own = b / per;              // the thread that counted it
-  const int n_total = tokens_of(b);
-  const int n = spans_of(n_total);
+  const int n_total = decode_position(ctx_lens[b], max_pages_per_seq) + 1;
+  const int n = (n_total + span_len - 1) / span_len;
   const int cl = last_class(n_total, n);
   int full_at = part[0][own], last_at = part[cl][own];
 #pragma unroll
   for (int c = 1; c < NB; ++c) last_at += c == cl ? class_base[c] : 0;
   for (int b2 = own * per; b2 < b; ++b2) {  // requests of the same thread in front of this one
-    const int t2 = tokens_of(b2), n2 = spans_of(t2);
+    const int t2 = decode_position(ctx_lens[b2], max_pages_per_seq) + 1, n2 = (t2 + span_len - 1) / span_len;
     full_at += n2 - 1;
     last_at += last_class(t2, n2) == cl ? 1 : 0;
   }
-  const int pages_per_span = span_len >> 4, last_page = (max(n_total, 1) - 1) / 16, first_page = prefix_of(b);
+  const int pages_per_span = span_len >> 4, last_page = (n_total - 1) / 16;
   auto at = [&](int k) { return k < n - 1 ? full_at + k : last_at; };
-  for (int k = lane; k < n; k += 64) items[at(k)] = make_int4(b, k, n_total, SHARED ? shared.spans(first_page) : 0);
+  for (int k = lane; k < n; k += 64) items[at(k)] = make_int4(b, k, n_total, 0);
   constexpr int UN = 4;
   for (int e0 = 0; e0 < n * pages_per_span; e0 += 64 * UN) {  // entry e is page e % pages_per_span of span e / pages_per_span
     int page[UN];
 #pragma unroll
     for (int u = 0; u < UN; ++u)
-      page[u] = block_tables[(int64_t)b * max_pages_per_seq + first_page + min(e0 + u * 64 + lane, last_page)];
+      page[u] = block_tables[(int64_t)b * max_pages_per_seq + min(e0 + u * 64 + lane, last_page)];
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
       const int e = e0 + u * 64 + lane;
@@ -150,10 +132,7 @@ __global__ __launch_bounds__(256) void attn_plan_kernel(const int32_t* __restric
 // (four pages) and the assignment of MFMA k-indices to channels (scores) and of score rows to
 // tokens changes with it; the arithmetic after the conversion is the bf16 kernel's.  The cache
 // scales ride along for free: k_scale in the softmax scale, v_scale in the final division.
-//
-// SHARED: a row's tokens behind the prefix that its group shares.  The prefix has been attended to by a kernel in front
-// (attn_prefix_kernel), whose partials, `it.w` spans of them, are combined with this row's own; a row without tokens gives zeros.
-template <int DH, bool KV8, bool ROTATE, bool SHARED>
+template <int DH, bool KV8, bool ROTATE>
 __global__ __launch_bounds__(256, 3) void attn_decode_kernel(const DecodeQueries dq, int batch,
                                                           int n_q_heads, KvLayout kv,
                                                           const int4* __restrict__ items,
@@ -533,9 +512,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_kernel(const DecodeQueries
     s_l[wave][r16] = lsum;
   }
   __syncthreads();
-  const int in_front = SHARED ? it.w : 0;  // spans of the prefix
-  const int own_spans = SHARED ? max(1, (n_total + span_len - 1) / span_len) : (n_total + span_len - 1) / span_len;
-  const int n_spans = in_front + own_spans;
+  const int n_spans = (n_total + span_len - 1) / span_len;
   for (int e = threadIdx.x; e < G * DH; e += 256) {
     const int q = e / DH, c = e % DH;
     const float m0 = s_m[0][q], m1 = s_m[1][q], m2 = s_m[2][q], m3 = s_m[3][q];
@@ -544,34 +521,10 @@ __global__ __launch_bounds__(256, 3) void attn_decode_kernel(const DecodeQueries
     const float num = w0 * s_o[0][q][c] + w1 * s_o[1][q][c] + w2 * s_o[2][q][c] + w3 * s_o[3][q][c];
     const float den = w0 * s_l[0][q] + w1 * s_l[1][q] + w2 * s_l[2][q] + w3 * s_l[3][q];
     const int h = kvh * G + q;
-    if (SHARED && own_spans == 1 && in_front > 0) {  // the prefix's spans and this one, in that order
-      constexpr int UN = 8;
-      const int64_t base = ((int64_t)b * n_q_heads + h) * max_spans;
-      float m_all = mt, num_all = 0.f, den_all = 0.f;
-      for (int k = 0; k < in_front; ++k) m_all = fmaxf(m_all, part_ml[(base + k) * 2]);
-      for (int k0 = 0; k0 < in_front; k0 += UN) {
-        float2 ml[UN];
-        float o1[UN];
-#pragma unroll
-        for (int u = 0; u < UN; ++u) {
-          const int64_t slot = base + min(k0 + u, in_front - 1);
-          ml[u] = *reinterpret_cast<const float2*>(part_ml + slot * 2);
-          o1[u] = part_o[slot * DH + c];
-        }
-#pragma unroll
-        for (int u = 0; u < UN; ++u) {
-          if (k0 + u >= in_front) break;
-          const float w = exp2f(ml[u].x - m_all);
-          den_all += w * ml[u].y;
-          num_all += w * o1[u];
-        }
-      }
-      const float w = exp2f(mt - m_all);
-      out[operand_offset(out_lay, b, h * DH + c)] = (bf16)((num_all + w * num) / (den_all + w * den) * out_scale);
-    } else if (n_spans == 1) {
-      out[operand_offset(out_lay, b, h * DH + c)] = (bf16)(SHARED && n_total <= 0 ? 0.f : num / den * out_scale);
+    if (n_spans == 1) {
+      out[operand_offset(out_lay, b, h * DH + c)] = (bf16)(num / den * out_scale);
     } else {
-      const int64_t slot = ((int64_t)b * n_q_heads + h) * max_spans + in_front + span;
+      const int64_t slot = ((int64_t)b * n_q_heads + h) * max_spans + span;
       if (spans_done) {
         store_agent(part_o + slot * DH + c, num);
         if (c == 0) {
@@ -587,7 +540,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_kernel(const DecodeQueries
       }
     }
   }
-  if ((SHARED ? own_spans : n_spans) == 1 || !spans_done) return;
+  if (n_spans == 1 || !spans_done) return;
   // ---- a request of several spans: whoever finishes last combines them, in the order of the spans whoever that is,
   //   out = sum_k o_k 2^(m_k - m) / sum_k l_k 2^(m_k - m).
   // The spans of a request are made on different XCDs, whose L2s do not see each other: partials are stored
@@ -601,7 +554,7 @@ __global__ __launch_bounds__(256, 3) void attn_decode_kernel(const DecodeQueries
   if (threadIdx.x == 0) {
     unsigned* done = spans_done + (int64_t)b * Hkv + kvh;
     const unsigned before = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = before + 1 == (unsigned)own_spans;
+    s_last = before + 1 == (unsigned)n_spans;
     if (s_last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
@@ -764,38 +717,29 @@ bool attn_decode_rotates(int batch, int n_kv_heads, int max_spans, int span_len)
 }
 
 hipError_t launch_attn_plan(const int32_t* ctx_lens, const int32_t* block_tables, int max_pages_per_seq, int batch,
-                            int max_spans, int span_len, int4* items, int32_t* item_pages, hipStream_t s, const SharedRows* shared) {
+                            int max_spans, int span_len, int4* items, int32_t* item_pages, hipStream_t s) {
   if (batch <= 0) return hipSuccess;
   const int max_items = attn_decode_items(batch, max_spans, span_len);
-  if (shared)
-    attn_plan_kernel<true><<<(batch + 3) / 4, 256, 0, s>>>(ctx_lens, batch, span_len, block_tables, max_pages_per_seq, items,
-                                                           max_items, item_pages, *shared);
-  else
-    attn_plan_kernel<false><<<(batch + 3) / 4, 256, 0, s>>>(ctx_lens, batch, span_len, block_tables, max_pages_per_seq, items,
-                                                            max_items, item_pages, SharedRows{});
+  attn_plan_kernel<<<(batch + 3) / 4, 256, 0, s>>>(ctx_lens, batch, span_len, block_tables, max_pages_per_seq, items,
+                                                  max_items, item_pages);
   return hipGetLastError();
 }
 
 hipError_t launch_attn_decode(const DecodeQueries& dq, int batch, int n_q_heads, const KvLayout& kv,
                               const int4* items, const int32_t* item_pages, int item_pitch, const int32_t* ctx_lens,
                               float* part_o, float* part_ml, unsigned* spans_done, int max_spans, int span_len,
-                              void* out, OperandLayout out_layout, hipStream_t s, bool shared) {
+                              void* out, OperandLayout out_layout, hipStream_t s) {
   if (batch <= 0) return hipSuccess;
   // 8-bit pools hold value / scale: the key scale joins the softmax scale, the value scale the final division
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)kv.head_dim) * (kv.fp8 ? kv.k_scale : 1.0f);
   const float out_scale = kv.fp8 ? kv.v_scale : 1.0f;
   const int max_items = attn_decode_items(batch, max_spans, span_len);
   const unsigned grid = (unsigned)max_items * kv.n_kv_heads;
-#define TDP_DECODE_(DH, KV8, ROTATE, SHARED)                                                                                   \
-  attn_decode_kernel<DH, KV8, ROTATE, SHARED><<<grid, 256, 0, s>>>(dq, batch, n_q_heads, kv, items, item_pages, item_pitch, ctx_lens, \
+#define TDP_DECODE_(DH, KV8, ROTATE)                                                                                   \
+  attn_decode_kernel<DH, KV8, ROTATE><<<grid, 256, 0, s>>>(dq, batch, n_q_heads, kv, items, item_pages, item_pitch, ctx_lens, \
                                                            part_o, part_ml, spans_done, max_spans, span_len, (bf16*)out, \
                                                            out_layout, scale_log2, out_scale)
-#define TDP_DECODE(DH, KV8)                                \
-  do {                                                     \
-    if (shared) TDP_DECODE_(DH, KV8, false, true);         \
-    else if (dq.qkv) TDP_DECODE_(DH, KV8, false, false);   \
-    else TDP_DECODE_(DH, KV8, true, false);                \
-  } while (0)
+#define TDP_DECODE(DH, KV8) do { if (dq.qkv) TDP_DECODE_(DH, KV8, false); else TDP_DECODE_(DH, KV8, true); } while (0)
   if (kv.head_dim == 128) {
     if (kv.fp8) TDP_DECODE(128, true); else TDP_DECODE(128, false);
   } else {

@@ -3,148 +3,635 @@
 //
 // What is shared is found in the tables, not told: a group is rows that may share something, and its prefix is the leading pages that are the
 // same in all of them, whole pages in front of every row's last token.  So the answer is that of ordinary decode attention whatever
-// the groups are.  Partials (reference m, sum l, unnormalised output o, per span of the prefix) go to the first slots of every row
-// and head; the decode kernel behind attends to what a row has of its own and combines all.
+// the groups are.  Three launches: the plan (once per step), the prefixes, the rows.  The prefix kernel leaves partials (reference m, sum
+// l, unnormalised output o, per span of the prefix) in the first slots of every row and head; a row's own kernel attends to what the row has
+// behind its prefix and combines all.
+#include <algorithm>
+
 #include "tdp_device.h"
 #include "tdp_kernels.h"
 
 namespace tdp {
 namespace {
 
-// Columns of a workgroup's tile: 128, or 64 or 32 where groups are small (two or four waves then share a block's tokens out).
-int tile_columns(int batch, int n_groups, int G) {
-  const int64_t average = ((int64_t)batch * G + n_groups - 1) / n_groups;
-  return average <= 32 ? 32 : average <= 64 ? 64 : 128;
-}
-// Spans wanted of one K/V head: the launch then has two to four workgroups for every one that the chip holds at once.
-int spans_wanted(int n_kv_heads) { return (1024 + n_kv_heads - 1) / n_kv_heads; }
-
 constexpr int kMinSpanPages = kDecodeSpanMin / 16;
+constexpr int kResident = 3 * 256;  // workgroups of the sixteen-column kernel that the chip holds at once
+
+// How a batch is attended to: a pure function of sizes that the host knows.
+struct Form {
+  int columns;      // of a tile of the prefix kernel: 16, 32, 64 or 128, by the average group
+  bool split;       // 16 columns: the waves of a workgroup share a span's tokens out, instead of taking a span each
+  int wanted;       // spans of the prefixes per K/V head (spans of a group times its tiles)
+};
+// Whether the waves of a workgroup share a row's span out as well.
+bool rows_split(int batch, int n_kv_heads) { return (int64_t)batch * n_kv_heads < 1024; }
+Form form_of(int batch, int n_groups, int n_q_heads, int n_kv_heads) {
+  const int G = n_q_heads / n_kv_heads;
+  const int64_t average = n_groups > 0 ? ((int64_t)batch * G + n_groups - 1) / n_groups : 0;
+  Form f;
+  f.columns = average <= 16 ? 16 : average <= 32 ? 32 : average <= 64 ? 64 : 128;
+  f.split = (int64_t)n_groups * n_kv_heads < 1024;
+  const int units = f.columns == 16 ? (f.split ? 2 * kResident : 8 * kResident) : f.columns == 32 ? 1024 : f.columns == 64 ? 1024 : 512;
+  f.wanted = (units + n_kv_heads - 1) / n_kv_heads;
+  return f;
+}
+int items_of(const SharedBatch& b, const Form& f) {
+  return (int)((int64_t)b.batch * (b.n_q_heads / b.n_kv_heads) / f.columns) + b.n_groups + f.wanted;
+}
 
 // ---- plan ------------------------------------------------------------------------------------------------------------------------
 
-// One workgroup per group: the pages that all its rows begin with.  Rows of length zero attend to nothing and do not count: what
-// their tables hold is not looked at, and the group's pages are those of its first row with tokens (group_first).
-__global__ __launch_bounds__(1024) void shared_prefix_kernel(const int32_t* __restrict__ group_starts, const int32_t* __restrict__ lens,
-                                                             const int32_t* __restrict__ block_tables, int max_pages_per_seq, int batch,
-                                                             const SharedRows rows, int32_t* __restrict__ row_pages,
-                                                             int32_t* __restrict__ group_pages, int32_t* __restrict__ group_first) {
-  __shared__ int most, longest, first, last;
-  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int begin = min(max(group_starts[g], 0), batch), end = min(max(group_starts[g + 1], begin), batch);
-  if (tid == 0) {
-    most = 0x7fffffff;
-    longest = 0;
-    first = end;
-    last = begin;
+struct PlanArgs {
+  SharedBatch b;
+  int columns, wanted, max_prefix_items;
+  int32_t* row_pages;  // [batch]: pages that a row has in common with the first of its group
+  int32_t* group;      // [4][n_groups], where they are too many for LDS
+  unsigned* done;
+  int32_t* counts;
+  int4 *prefix_items, *row_items;
+};
+constexpr int kPlanThreads = 256, kPlanRows = 32;  // rows that a workgroup compares, as long as there are not too many workgroups
+constexpr int kPlanHeld = 1024;                    // rows, and groups, that the last workgroup holds in LDS
+constexpr int kClasses = 17;                       // of row spans by their length
+__device__ __forceinline__ int row_tokens(const SharedBatch& b, int r) { return min(max(b.lens[r], 0) + b.add, b.max_pages_per_seq * 16); }
+
+// A thread's value plus those of all threads of the workgroup in front of it, and the sum of all.
+__device__ __forceinline__ int plan_scan(int v, int* part, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int up = __shfl_up(v, o, 64);
+    if (lane >= o) v += up;
   }
+  __syncthreads();  // (part may still be read)
+  if (lane == 63) part[wave] = v;
   __syncthreads();
-  for (int r = begin + tid; r < end; r += 1024) {
-    const int n = rows.tokens(lens[r], max_pages_per_seq);
-    if (n > 0) {
-      atomicMin(&most, (n - 1) >> 4);
-      atomicMax(&longest, n);
-      atomicMin(&first, r);
-      atomicMax(&last, r);
-    }
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    v += w < wave ? part[w] : 0;
+    all += part[w];
   }
-  __syncthreads();
-  // the first difference between any row and the first of them; a wave compares four rows' 256 entries at a time
-  const int limit = most, r0 = first, others = last - r0;  // (0: one row with tokens, or none)
-  __syncthreads();
-  if (others < 1) {
-    if (tid == 0) most = 0;
-  } else {
-    constexpr int ROWS = 4, PART = 4;
-    const int chunks = (limit + 64 * PART - 1) / (64 * PART), fours = (others + ROWS - 1) / ROWS;
-    const int32_t* const base = block_tables + (int64_t)r0 * max_pages_per_seq;
-    for (int i = wave; i < fours * chunks; i += 16) {
-      const int c = i / fours, r = r0 + 1 + (i - c * fours) * ROWS;  // (low pages first)
-      const int at = c * 64 * PART + lane;
-      if (c * 64 * PART >= *(volatile int*)&most) break;
-      int want[PART], got[ROWS][PART];
-      bool in[ROWS];
-#pragma unroll
-      for (int u = 0; u < PART; ++u) want[u] = base[min(at + u * 64, limit - 1)];
-#pragma unroll
-      for (int j = 0; j < ROWS; ++j) {
-        const int row = min(r + j, r0 + others);
-        in[j] = rows.tokens(lens[row], max_pages_per_seq) > 0;
-#pragma unroll
-        for (int u = 0; u < PART; ++u) got[j][u] = block_tables[(int64_t)row * max_pages_per_seq + min(at + u * 64, limit - 1)];
-      }
-      int differs = 0x7fffffff;
-#pragma unroll
-      for (int u = PART - 1; u >= 0; --u)
-#pragma unroll
-        for (int j = 0; j < ROWS; ++j)
-          if (in[j] && got[j][u] != want[u]) differs = min(at + u * 64, limit - 1);
-      if (differs < limit) atomicMin(&most, differs);
-    }
+  *total = all;
+  return v;
+}
+// The last i in [0, n) with at[i] <= v (at ascending; 0 if there is none).
+__device__ __forceinline__ int last_not_above(const int32_t* at, int n, int v) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (at[mid] <= v) lo = mid; else hi = mid - 1;
   }
-  __syncthreads();
-  // A short prefix is left to the rows where one of them has more than the shortest span behind it: there is little to save, and a row has
-  // no more slots for partials than spans of that length.
-  const int found = most;
-  const int pages = found < kMinSpanPages && longest - found * 16 > kDecodeSpanMin ? 0 : found;
-  for (int r = begin + tid; r < end; r += 1024) row_pages[r] = pages;
-  if (tid == 0) {
-    group_pages[g] = pages;
-    group_first[g] = r0;
-  }
+  return lo;
 }
 
-// The work list of the prefix kernel: an item is a span of a group's prefix and a tile of its columns, two records
-//   (first row, first column, columns of the group, span), (first page, pages, row whose table names them, 0),
-// and (-1, ...) behind the last.  Spans are as long as the number wanted allows, and all of a group equally long.
-__global__ __launch_bounds__(1024) void shared_list_kernel(const int32_t* __restrict__ group_starts, int n_groups, int batch, int G, int columns,
-                                                           int wanted, const int32_t* __restrict__ group_pages, const int32_t* __restrict__ group_first,
-                                                           int32_t* __restrict__ span_pages, int4* __restrict__ items, int max_items) {
-  __shared__ long long work;
-  __shared__ int part[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  auto tiles_of = [&](int g) {
-    const int begin = min(max(group_starts[g], 0), batch), end = min(max(group_starts[g + 1], begin), batch);
-    return ((end - begin) * G + columns - 1) / columns;
+// Workgroups compare tables, each those of a range of rows; the one that finishes last makes both work lists (prefix items: two records
+//   (first row of the group, first column, columns of the group, span), (first page, pages, row whose table names them, 0);
+// row items: (row, pages of the prefix, tokens behind it, span | spans of the prefix << 16)).  Results of other workgroups, which run on
+// other XCDs, are stored and read past the caches, and counted when they have arrived.
+// Rows of length zero attend to nothing: what their tables hold is not looked at.
+// Bound: a chain of look-ups and barriers (a workgroup alone: 5 us), and the tables, which one CU reads at some 30 GB/s.
+__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArgs a) {
+  constexpr int T = kPlanThreads;
+  __shared__ int32_t s_starts[kPlanHeld + 1], s_tokens[kPlanHeld], s_group[4 * kPlanHeld], s_pages[T], s_first[T];
+  __shared__ int is_last, longest_limit, part[T / 64], class_at[kClasses];
+  __shared__ unsigned work;
+  const SharedBatch& b = a.b;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, P = b.max_pages_per_seq, n_groups = b.n_groups;
+  const bool few = n_groups <= kPlanHeld, held = b.batch <= kPlanHeld;
+  if (few && n_groups > 0)
+    for (int g = tid; g <= n_groups; g += T) s_starts[g] = b.group_starts[g];
+  if (held)
+    for (int r = tid; r < b.batch; r += T) s_tokens[r] = row_tokens(b, r);
+  auto tokens_of = [&](int r) { return held ? s_tokens[r] : row_tokens(b, r); };
+  const int32_t* const starts = few ? s_starts : b.group_starts;
+  // the group of a row, or -1: [begin, end) of a group, in bounds whatever the starts are
+  auto begin_of = [&](int g) { return min(max(starts[g], 0), b.batch); };
+  auto end_of = [&](int g) { return min(max(starts[g + 1], begin_of(g)), b.batch); };
+  auto group_of = [&](int r) {
+    if (n_groups == 0) return -1;
+    const int g = last_not_above(starts, n_groups, r);
+    return r >= begin_of(g) && r < end_of(g) ? g : -1;
   };
+  if (n_groups > 0) {
+    const int each = (b.batch + gridDim.x - 1) / gridDim.x, own_begin = min((int)blockIdx.x * each, b.batch), own_end = min(own_begin + each, b.batch);
+    for (int t0 = own_begin; t0 < own_end; t0 += T) {
+      const int rows = min(own_end - t0, T);
+      if (tid == 0) longest_limit = 0;
+      __syncthreads();  // (starts are there; the tile before is done with)
+      if (tid < rows) {
+        // as many pages as a row has in front of its last token, and the first row of its group that has some; -1: no tokens, or no group
+        const int r = t0 + tid, g = group_of(r), own_tokens = tokens_of(r);
+        int first = r, limit = -1;
+        if (g >= 0 && own_tokens > 0) {
+          limit = (own_tokens - 1) >> 4;
+          int tokens = 0;
+          for (first = begin_of(g); first < r && (tokens = tokens_of(first)) <= 0;) ++first;
+          if (first < r) {
+            limit = min(limit, (tokens - 1) >> 4);
+            atomicMax(&longest_limit, limit);
+          }
+        }
+        s_pages[tid] = limit;
+        s_first[tid] = first;
+      }
+      __syncthreads();
+      // the first difference from that row: a wave compares eight rows' 256 entries at a time, low pages first
+      constexpr int ROWS = 8, PART = 4;
+      const int chunks = (longest_limit + 64 * PART - 1) / (64 * PART), eights = (rows + ROWS - 1) / ROWS;
+      for (int i = wave; i < eights * chunks; i += T / 64) {
+        const int c = i / eights, at = c * 64 * PART + lane, row0 = (i - c * eights) * ROWS;
+        int limit[ROWS], want[ROWS][PART], got[ROWS][PART];
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+          const int row = min(row0 + j, rows - 1), of = s_first[row];
+          limit[j] = of == t0 + row ? 0 : *(volatile int*)&s_pages[row];
+#pragma unroll
+          for (int u = 0; u < PART; ++u) {  // (in bounds, and not used where a row has nothing to compare)
+            const int e = min(at + u * 64, max(limit[j], 1) - 1);
+            want[j][u] = b.block_tables[(int64_t)of * P + e];
+            got[j][u] = b.block_tables[(int64_t)(t0 + row) * P + e];
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+          int differs = 0x7fffffff;
+#pragma unroll
+          for (int u = PART - 1; u >= 0; --u)
+            if (got[j][u] != want[j][u]) differs = min(at + u * 64, limit[j] - 1);
+          if (differs < limit[j]) atomicMin(&s_pages[min(row0 + j, rows - 1)], differs);
+        }
+      }
+      __syncthreads();
+      if (tid < rows) store_agent(a.row_pages + t0 + tid, s_pages[tid]);
+    }
+    if (gridDim.x > 1) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (tid == 0) {
+        const unsigned before = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        is_last = before + 1 == gridDim.x;
+        if (is_last) __hip_atomic_store(a.done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      if (!is_last) return;
+    }
+  }
+  const bool in_lds = gridDim.x == 1 && b.batch <= T;  // what has been found out of the rows
+  auto pages_of = [&](int r) { return in_lds ? s_pages[r] : load_agent(a.row_pages + r); };
+  if (!in_lds) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (alone, with several tiles: its own stores)
+  // What the groups share, and how much there is to do for it: [n_groups] each of pages, longest row, first and last row with tokens.
+  int32_t* const common = few ? s_group : a.group;
+  const int pitch = few ? kPlanHeld : n_groups;
+  int32_t *const longest = common + pitch, *const first = longest + pitch, *const last = first + pitch;
+  int32_t* const spans = longest;  // (then) spans of the prefix
   if (tid == 0) work = 0;
+  if (tid < kClasses) class_at[tid] = 0;
+  for (int g = tid; g < n_groups; g += T) {
+    common[g] = first[g] = 0x7fffffff;
+    longest[g] = 0;
+    last[g] = -1;
+  }
   __syncthreads();
-  for (int g = tid; g < n_groups; g += 1024)
-    atomicAdd((unsigned long long*)&work, (unsigned long long)tiles_of(g) * (unsigned long long)group_pages[g]);
+  for (int r = tid; n_groups > 0 && r < b.batch; r += T) {
+    const int g = group_of(r), pages = g >= 0 ? pages_of(r) : -1;
+    if (pages >= 0) {
+      atomicMin(common + g, pages);
+      atomicMax(longest + g, tokens_of(r));
+      atomicMin(first + g, r);
+      atomicMax(last + g, r);
+    }
+  }
   __syncthreads();
-  const int span = (int)max((long long)kMinSpanPages, (work + wanted - 1) / wanted);
-  if (tid == 0) *span_pages = span;
+  auto tiles_of = [&](int g) { return ((end_of(g) - begin_of(g)) * (b.n_q_heads / b.n_kv_heads) + a.columns - 1) / a.columns; };
+  for (int g = tid; g < n_groups; g += T) {
+    int pages = common[g];
+    // A short prefix is left to the rows where one of them has more than the shortest span behind it: there is little to save, and a row
+    // has no more slots for partials than spans of that length.
+    if (last[g] <= first[g] || (pages < kMinSpanPages && longest[g] - pages * 16 > kDecodeSpanMin)) pages = 0;
+    common[g] = pages;
+    if (pages) atomicAdd(&work, (unsigned)tiles_of(g) * pages);  // (below 2^32: no more rows than pages of 32 bits name)
+  }
+  __syncthreads();
+  // prefixes in spans as long as the number wanted allows, all of a group equally long; their items, a thread each
+  const int span = max((unsigned)kMinSpanPages, (work + a.wanted - 1) / a.wanted);
+  auto spans_of = [&](int pages) { return pages > 0 ? max(1, min((pages + span - 1) / span, pages / kMinSpanPages)) : 0; };
   int base = 0;
-  for (int g0 = 0; g0 < n_groups; g0 += 1024) {
-    const int g = g0 + tid, pages = g < n_groups ? group_pages[g] : 0;
-    const int spans = pages > 0 ? max(1, pages / span) : 0, tiles = spans ? tiles_of(g) : 0, own = spans * tiles;
-    int at = own;
+  for (int g0 = 0; g0 < n_groups; g0 += T) {
+    const int g = g0 + tid, pages = g < n_groups ? common[g] : 0;
+    const int own_spans = spans_of(pages), n = own_spans ? own_spans * tiles_of(g) : 0;
+    int total;
+    const int behind = plan_scan(n, part, &total);
+    s_first[tid] = behind - n;
+    if (g < n_groups) spans[g] = own_spans;
+    __syncthreads();
+    for (int i = tid; i < total && base + i < a.max_prefix_items; i += T) {
+      const int at = last_not_above(s_first, min(n_groups - g0, T), i), of = g0 + at;  // (the last that begins there is the one that has some)
+      const int row = begin_of(of), tiles = tiles_of(of), own = i - s_first[at];
+      const unsigned s = own / tiles, from = s * (unsigned)common[of] / spans[of], to = (s + 1) * (unsigned)common[of] / spans[of];
+      a.prefix_items[2 * (base + i)] = make_int4(row, (own - s * tiles) * a.columns, (end_of(of) - row) * (b.n_q_heads / b.n_kv_heads), s);
+      a.prefix_items[2 * (base + i) + 1] = make_int4(from, to - from, first[of], 0);
+    }
+    base += total;
+    __syncthreads();
+  }
+  if (tid == 0) a.counts[0] = min(base, a.max_prefix_items);
+  // The rows' spans, longest first by sixteenths of span_len, so that the launch ends on short ones: counted per class, then placed.  (In no
+  // fixed order within a class; a row's result does not depend on its place.)
+  struct Row {
+    int pages, tokens, spans, in_front;
+  };
+  auto row_of = [&](int r) {
+    Row x{0, tokens_of(r), 0, 0};
+    const int g = x.tokens > 0 ? group_of(r) : -1;
+    if (g >= 0) {
+      x.pages = common[g];
+      x.in_front = x.pages ? spans[g] : 0;
+    }
+    x.tokens -= x.pages * 16;
+    x.spans = max(1, (x.tokens + b.span_len - 1) / b.span_len);
+    return x;
+  };
+  auto class_of = [&](const Row& x) {  // of the last span; 0: whole spans
+    const int tokens = x.tokens - (x.spans - 1) * b.span_len;
+    return kClasses - 1 - max(0, tokens - 1) / (b.span_len / (kClasses - 1));
+  };
+  Row own{0, 0, 0, 0};
+  for (int r = tid; r < b.batch; r += T) {
+    own = row_of(r);
+    if (own.spans > 1) atomicAdd(&class_at[0], own.spans - 1);
+    atomicAdd(&class_at[class_of(own)], 1);
+  }
+  __syncthreads();
+  if (tid < 64) {
+    const int n = tid < kClasses ? class_at[tid] : 0;
+    int at = n;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
       const int up = __shfl_up(at, o, 64);
-      if (lane >= o) at += up;
+      if (tid >= o) at += up;
     }
-    __syncthreads();
-    if (lane == 63) part[wave] = at;
-    __syncthreads();
-    int all = 0;
-    at += base - own;
-    for (int w = 0; w < 16; ++w) {
-      at += w < wave ? part[w] : 0;
-      all += part[w];
-    }
-    const int row = own ? min(max(group_starts[g], 0), batch) : 0, end = own ? min(max(group_starts[g + 1], row), batch) : 0;
-    for (int i = 0; i < own && at + i < max_items; ++i) {
-      const int s = i / tiles, first = (int)((int64_t)s * pages / spans);
-      items[2 * (at + i)] = make_int4(row, (i - s * tiles) * columns, (end - row) * G, s);
-      items[2 * (at + i) + 1] = make_int4(first, (int)((int64_t)(s + 1) * pages / spans) - first, group_first[g], 0);
-    }
-    base += all;
+    if (tid < kClasses) class_at[tid] = at - n;
+    if (tid == kClasses - 1) a.counts[1] = at;
   }
-  for (int i = base + tid; i < max_items; i += 1024) items[2 * i] = make_int4(-1, 0, 0, 0);
+  __syncthreads();
+  for (int r = tid; r < b.batch; r += T) {
+    if (b.batch > T) own = row_of(r);
+    const int at = own.spans > 1 ? atomicAdd(&class_at[0], own.spans - 1) : 0, last_at = atomicAdd(&class_at[class_of(own)], 1);
+    for (int k = 0; k < own.spans; ++k)
+      a.row_items[k + 1 < own.spans ? at + k : last_at] = make_int4(r, own.pages, own.tokens, k | own.in_front << 16);
+  }
 }
 
-// ---- attention to the prefix -----------------------------------------------------------------------------------------------------
+// ---- sixteen columns -------------------------------------------------------------------------------------------------------------
+
+// Attention of up to sixteen columns to a span of pages, keys and values from memory straight into MFMA operands, as in decode attention: the
+// columns are the 16-wide side of 16x16x32 MFMAs, scores are formed transposed, and their rows are assigned to tokens so that a lane's elements
+// are the consecutive tokens that it supplies to O^T += V^T P^T.
+//
+// PREFIX: the columns are (row, head) pairs of a group, the span one of its prefix; the partials go to the columns' slots.  Otherwise they are the
+// heads of one row, the span one of what it has behind its prefix; the prefix's partials, and those of the row's other spans if it has some
+// (whoever is done last), are combined with them.
+// SPLIT: the four waves of a workgroup share the span out; otherwise each has one of its own, with no LDS and no barrier: short spans by
+// the thousand are mostly their own beginning and end.
+template <int DH, bool KV8, bool PREFIX, bool SPLIT>
+__global__ __launch_bounds__(256, KV8 && DH == 128 ? 2 : 3) void attn_columns_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
+                                                              const int4* __restrict__ items, const int32_t* __restrict__ count,
+                                                              const int32_t* __restrict__ block_tables, int max_pages_per_seq,
+                                                              float* __restrict__ part_o, float* __restrict__ part_ml,
+                                                              unsigned* __restrict__ spans_done, int max_spans, int span_len,
+                                                              bf16* __restrict__ out, OperandLayout out_lay, float scale_log2, float out_scale) {
+  constexpr int KS = DH / 32;        // k-steps of the score MFMA
+  constexpr int DT = DH / 16;        // 16-channel tiles of the output
+  constexpr int BT = KV8 ? 64 : 32;  // tokens per block
+  constexpr int NT = BT / 16;        // score tiles per block
+  constexpr int NP = BT / 32;        // k-steps of the output MFMA per block
+  constexpr int LT = BT / 4;         // consecutive tokens of a block whose scores end up in one lane
+  constexpr int kChunk = 256;        // pages whose ids the wave holds at once, four to a lane
+  constexpr int PITCH = DT * 4 + 2;
+  __shared__ float s_state[SPLIT ? 3 * 64 * PITCH : 1];
+  const int Hkv = kv.n_kv_heads, G = n_q_heads / Hkv;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, kg = lane >> 4;
+  const bf16* const kpool = (const bf16*)kv.k_pool;
+  const bf16* const vpool = (const bf16*)kv.v_pool;
+  const uint8_t* const kpool8 = (const uint8_t*)kv.k_pool;
+  const uint8_t* const vpool8 = (const uint8_t*)kv.v_pool;
+  const int krow0 = (r16 >> 2) * LT + (r16 & 3);  // token (within a block) of this lane's row in score tile t: krow0 + t * 4
+  const int units = *count * Hkv, stride = SPLIT ? gridDim.x : gridDim.x * 4;
+  for (int unit = SPLIT ? blockIdx.x : blockIdx.x * 4 + wave; unit < units; unit += stride) {
+    const int item = unit / Hkv, kvh = unit - item * Hkv;
+    // the lane's column of an item
+    struct Column {
+      int row, head;
+      bool real;
+    };
+    auto column_of = [&](int4 x) {
+      if constexpr (PREFIX) {
+        const int col = x.y + r16, c = min(col, x.z - 1), r = c / G;
+        return Column{x.x + r, kvh * G + c - r * G, col < x.z};
+      } else {
+        return Column{x.x, kvh * G + min(r16, G - 1), r16 < G};
+      }
+    };
+    int tokens;
+    const int32_t* table;
+    bf16x8 qf[KS];
+    {
+      const int4 x = items[PREFIX ? 2 * item : item];
+      if constexpr (PREFIX) {
+        const int4 y = items[2 * item + 1];
+        tokens = y.y * 16;
+        table = block_tables + (int64_t)y.z * max_pages_per_seq + y.x;
+      } else {
+        const int begin = (x.w & 0xffff) * span_len;
+        tokens = min(x.z - begin, span_len);
+        table = block_tables + (int64_t)x.x * max_pages_per_seq + x.y + begin / 16;
+      }
+      // Query fragments.  bf16 pools: k-step kk covers channels kk*32 + kg*8 .. +8.  8-bit pools: a lane's 16-byte key load covers channels
+      // ld*64 + kg*16 .. +16, whose halves feed k-steps 2 ld and 2 ld + 1, so the query is gathered in that order.
+      const Column c = column_of(x);
+      const bf16* qp = q + (int64_t)c.row * ld + (int64_t)c.head * DH;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) qf[kk] = ld_bf16x8(qp + (KV8 ? (kk >> 1) * 64 + kg * 16 + (kk & 1) * 8 : kk * 32 + kg * 8));
+    }
+    f32x4 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = kNegBig, lsum = 0.f;
+
+    for (int c0 = 0; c0 < tokens; c0 += kChunk * 16) {
+      const int n_total = min(tokens - c0, kChunk * 16), last_entry = (n_total - 1) >> 4;
+      int my_pages[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) my_pages[j] = table[(c0 >> 4) + min(lane + 64 * j, last_entry)];
+      const int n_blocks = (n_total + BT - 1) / BT;
+      const int t_begin = SPLIT ? BT * ((wave * n_blocks) >> 2) : 0;
+      const int t_end = SPLIT ? min(BT * (((wave + 1) * n_blocks) >> 2), n_total) : n_total;
+      if (t_begin >= t_end) continue;
+      auto page_of = [&](int i) -> int64_t {  // i is wave-uniform
+        const int r = i >> 6;
+        return __builtin_amdgcn_readlane(r == 0 ? my_pages[0] : r == 1 ? my_pages[1] : r == 2 ? my_pages[2] : my_pages[3], i & 63);
+      };
+      struct KBlock {
+        bf16x8 kf[2][KS];  // bf16: [score tile][k-step]; 8 bits: 16 raw bytes per entry, [t / 2][(t % 2) * KS/2 + ld]
+      };
+      struct VBlock {
+        bf16x8 vf[DT];     // bf16: 8 tokens of a channel; 8 bits: 16 raw bytes = 16 tokens of a channel
+      };
+      auto load_k = [&](int tb, KBlock& blk) {
+        int64_t page[BT / 16];
+#pragma unroll
+        for (int j = 0; j < BT / 16; ++j) page[j] = page_of(min((tb >> 4) + j, last_entry));
+        if constexpr (KV8) {
+          const int64_t kpage = (r16 >> 2) == 0 ? page[0] : (r16 >> 2) == 1 ? page[1] : (r16 >> 2) == 2 ? page[2] : page[3];
+          const uint8_t* kp = kpool8 + (kpage * Hkv + kvh) * (16 * DH) + (r16 & 3) * 64 + kg * 16;
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int l = 0; l < KS / 2; ++l)
+              blk.kf[t >> 1][(t & 1) * (KS / 2) + l] = ld_bf16x8_nt(reinterpret_cast<const bf16*>(kp + (t * 4) * 64 + l * 1024));
+        } else {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const int tok = krow0 + t * 4;
+            const bf16* kp = kpool + (page[tok >> 4 & 1] * Hkv + kvh) * (16 * DH) + (tok & 15) * 32 + kg * 8;
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) blk.kf[t][kk] = ld_bf16x8_nt(kp + kk * (16 * 32));
+          }
+        }
+      };
+      auto load_v = [&](int tb, VBlock& blk) {
+        int64_t page[BT / 16];
+#pragma unroll
+        for (int j = 0; j < BT / 16; ++j) page[j] = page_of(min((tb >> 4) + j, last_entry));
+        if constexpr (KV8) {
+          const int64_t vpage = kg == 0 ? page[0] : kg == 1 ? page[1] : kg == 2 ? page[2] : page[3];
+          const uint8_t* vp = vpool8 + ((vpage * Hkv + kvh) * DH + r16) * 16;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) blk.vf[d] = ld_bf16x8_nt(reinterpret_cast<const bf16*>(vp + d * 16 * 16));
+        } else {
+          const int64_t vpage = kg < 2 ? page[0] : page[1];
+          const bf16* vp = vpool + ((vpage * Hkv + kvh) * DH + r16) * 16 + (kg & 1) * 8;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) blk.vf[d] = ld_bf16x8_nt(vp + d * 16 * 16);
+        }
+      };
+      auto compute_block = [&](int tb, KBlock& blk, VBlock& vblk) {
+        f32x4 s[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if constexpr (KV8) {
+#pragma unroll
+            for (int l = 0; l < KS / 2; ++l) {
+              bf16x8 k0, k1;
+              e4m3x16_to_bf16x8x2(__builtin_bit_cast(uint4, blk.kf[t >> 1][(t & 1) * (KS / 2) + l]), k0, k1);
+              s[t] = mfma16(k0, qf[2 * l], s[t]);
+              s[t] = mfma16(k1, qf[2 * l + 1], s[t]);
+            }
+          } else {
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) s[t] = mfma16(blk.kf[t][kk], qf[kk], s[t]);
+          }
+        }
+        // lane holds tokens tb + kg*LT + t*4 + i of column r16
+        const int tok_base = tb + kg * LT;
+        float mx = kNegBig;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = (tok_base + t * 4 + i < n_total) ? s[t][i] * scale_log2 : kNegBig;
+            s[t][i] = v;
+            mx = fmaxf(mx, v);
+          }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(m, mx);
+        const float alpha = exp2f(m - m_new);
+        bf16x8 pb[NP];
+        float psum = 0.f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float pv = exp2f(s[t][i] - m_new);
+            psum += pv;
+            pb[t >> 1][(t & 1) * 4 + i] = (bf16)pv;  // (rounded for the MFMA alone: the sum is of what it was)
+          }
+        lsum = lsum * alpha + psum;
+        m = m_new;
+        const bool tail = tb + BT > n_total;  // slots behind the span may hold anything, even NaN
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          o[d] *= alpha;
+          if constexpr (KV8) {
+            uint4 raw = __builtin_bit_cast(uint4, vblk.vf[d]);
+            if (tail) {  // keep the first n_total - tok_base bytes (tokens tok_base .. tok_base + 15)
+              const int keep = min(max(n_total - tok_base, 0), 16);
+              auto mask = [&](int w) -> uint32_t {
+                const int k4 = min(max(keep - 4 * w, 0), 4);
+                return k4 == 4 ? 0xffffffffu : (1u << (8 * k4)) - 1u;
+              };
+              raw.x &= mask(0);
+              raw.y &= mask(1);
+              raw.z &= mask(2);
+              raw.w &= mask(3);
+            }
+            bf16x8 v0, v1;
+            e4m3x16_to_bf16x8x2(raw, v0, v1);
+            o[d] = mfma16(v0, pb[0], o[d]);
+            o[d] = mfma16(v1, pb[NP - 1], o[d]);
+          } else {
+            if (tail) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (tok_base + j >= n_total) vblk.vf[d][j] = (bf16)0.0f;
+            }
+            o[d] = mfma16(vblk.vf[d], pb[0], o[d]);
+          }
+        }
+      };
+      // Keys a block ahead in one of two register sets, values into one set at the start of the block's own turn; every block is loaded once.
+      KBlock k0, k1;
+      VBlock v;
+      int tb = t_begin;
+      load_k(tb, k0);
+      for (; tb + 2 * BT < t_end; tb += 2 * BT) {
+        load_v(tb, v);
+        load_k(tb + BT, k1);
+        compute_block(tb, k0, v);
+        load_v(tb + BT, v);
+        load_k(tb + 2 * BT, k0);
+        compute_block(tb + BT, k1, v);
+      }
+      if (tb + BT < t_end) {
+        load_v(tb, v);
+        load_k(tb + BT, k1);
+        compute_block(tb, k0, v);
+        load_v(tb + BT, v);
+        compute_block(tb + BT, k1, v);
+      } else {
+        load_v(tb, v);
+        compute_block(tb, k0, v);
+      }
+    }
+    lsum += __shfl_xor(lsum, 16, 64);
+    lsum += __shfl_xor(lsum, 32, 64);
+
+    // one more state of this lane's column, wherever it comes from
+    auto join = [&](float m2, float l2, auto o_of) {
+      const float m_new = fmaxf(m, m2), mine = exp2f(m - m_new), its = exp2f(m2 - m_new);
+      m = m_new;
+      lsum = lsum * mine + l2 * its;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const f32x4 x = o_of(d);
+        o[d] = o[d] * mine + x * its;
+      }
+    };
+    if constexpr (SPLIT) {  // the other waves' states, in order
+      __syncthreads();  // (of the unit before have been read)
+      if (wave > 0) {
+        float* const at = s_state + ((wave - 1) * 64 + lane) * PITCH;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) *reinterpret_cast<float2*>(at + d * 4 + i) = make_float2(o[d][i], o[d][i + 1]);
+        *reinterpret_cast<float2*>(at + DT * 4) = make_float2(m, lsum);
+      }
+      __syncthreads();
+      if (wave > 0) continue;
+#pragma unroll
+      for (int w = 0; w < 3; ++w) {
+        const float* const at = s_state + (w * 64 + lane) * PITCH;
+        const float2 ml = *reinterpret_cast<const float2*>(at + DT * 4);
+        join(ml.x, ml.y, [&](int d) {
+          const float2 x = *reinterpret_cast<const float2*>(at + d * 4), y = *reinterpret_cast<const float2*>(at + d * 4 + 2);
+          return f32x4{x.x, x.y, y.x, y.y};
+        });
+      }
+    }
+    // (the item is read again: what it says would hold registers through all of the above)
+    int item_again = item;
+    asm volatile("" : "+s"(item_again));
+    const int4 it = items[PREFIX ? 2 * item_again : item_again];
+    const Column c = column_of(it);
+    const int row = c.row, head = c.head;
+    const bool real = c.real;
+    const int in_front = PREFIX ? 0 : it.w >> 16, slot = PREFIX ? it.w : in_front + (it.w & 0xffff);
+    const int own_spans = PREFIX ? 1 : max(1, (it.z + span_len - 1) / span_len);
+    const int64_t base = ((int64_t)row * n_q_heads + head) * max_spans;
+    float* const o_at = part_o + base * DH + kg * 4;  // channels d * 16 + kg * 4 + i of slot 0
+    if constexpr (PREFIX) {
+      if (real) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(o_at + (int64_t)slot * DH + d * 16) = o[d];
+        if (kg == 0) *reinterpret_cast<float2*>(part_ml + (base + slot) * 2) = make_float2(m, lsum);
+      }
+    } else {
+      if (own_spans > 1) {
+        // The spans of a row are made on different XCDs, whose L2s do not see each other: partials are stored and read past them, the wave waits
+        // until its stores have arrived, and only then is the span counted.  The last one puts the counter back for the next launch.
+        if (real) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) store_agent(o_at + (int64_t)slot * DH + d * 16 + i, o[d][i]);
+          if (kg == 0) {
+            store_agent(part_ml + (base + slot) * 2, m);
+            store_agent(part_ml + (base + slot) * 2 + 1, lsum);
+          }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        unsigned before = 0;
+        unsigned* const done = spans_done + (int64_t)row * Hkv + kvh;
+        if (lane == 0) before = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        before = __builtin_amdgcn_readfirstlane(before);
+        if (before + 1 != (unsigned)own_spans) continue;
+        if (lane == 0) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        m = kNegBig;
+        lsum = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      // in the order of the spans, whoever is last (a row's only span, in registers, first)
+      for (int k = 0; k < in_front; ++k) {
+        const float* const from = o_at + (int64_t)k * DH;
+        const float2 ml = *reinterpret_cast<const float2*>(part_ml + (base + k) * 2);
+        f32x4 x[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) x[d] = *reinterpret_cast<const f32x4*>(from + d * 16);
+        join(ml.x, ml.y, [&](int d) { return x[d]; });
+      }
+      if (own_spans > 1)
+        for (int k = in_front; k < in_front + own_spans; ++k) {
+          const float* const from = o_at + (int64_t)k * DH;
+          const float2 ml = load_agent2(part_ml + (base + k) * 2);
+          f32x4 x[DT];
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const float2 lo = load_agent2(from + d * 16), hi = load_agent2(from + d * 16 + 2);
+            x[d] = f32x4{lo.x, lo.y, hi.x, hi.y};
+          }
+          join(ml.x, ml.y, [&](int d) { return x[d]; });
+        }
+      if (real) {
+        const float scale = it.z > 0 ? out_scale / lsum : 0.f;  // (a row without tokens gives zeros)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          bf16x4 v4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v4[i] = (bf16)(o[d][i] * scale);
+          *reinterpret_cast<bf16x4*>(out + operand_offset(out_lay, row, head * DH + d * 16 + kg * 4)) = v4;
+        }
+      }
+    }
+  }
+}
+
+// ---- many columns ------------------------------------------------------------------------------------------------------------
 
 // One workgroup of four waves per (item, K/V head).  NWC waves have 32 columns each, and 4 / NWC waves share the tokens of a block out for
 // the same columns.  A block of 64 tokens (128 for one wave of columns) of K and V^T is staged in LDS, double buffered and swizzled,
@@ -153,7 +640,7 @@ __global__ __launch_bounds__(1024) void shared_list_kernel(const int32_t* __rest
 // Bound: reading the pages up to about a hundred columns, MFMA beyond.
 template <int DH, int NWC, bool KV8>
 __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
-                                                                            const int4* __restrict__ items,
+                                                                            const int4* __restrict__ items, const int32_t* __restrict__ count,
                                                                             const int32_t* __restrict__ block_tables, int max_pages_per_seq,
                                                                             float* __restrict__ part_o, float* __restrict__ part_ml,
                                                                             int max_spans, float scale_log2) {
@@ -171,9 +658,8 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
 
   const int Hkv = kv.n_kv_heads, G = n_q_heads / Hkv;
   const int item = blockIdx.x / Hkv, kvh = blockIdx.x - item * Hkv;
-  const int4 it = items[2 * item];
-  if (it.x < 0) return;
-  const int4 it2 = items[2 * item + 1];
+  if (item >= *count) return;
+  const int4 it = items[2 * item], it2 = items[2 * item + 1];
   const int first_page = it2.x, n_pages = it2.y, n_tokens = n_pages * 16;
   const int32_t* const table = block_tables + (int64_t)it2.z * max_pages_per_seq + first_page;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -182,13 +668,19 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
   const int wc = w % NWC, wt = w / NWC;
 
   // the lane's column; columns behind the last are computed as the last one and never stored
-  const int col = it.y + wc * 32 + l32;
-  const bool real = col < it.z;
-  const int c = min(col, it.z - 1), row = it.x + c / G, head = kvh * G + c % G;
+  struct Column {
+    int row, head;
+    bool real;
+  };
+  auto column_of = [&](int4 x) {
+    const int col = x.y + wc * 32 + l32, c = min(col, x.z - 1), r = c / G;
+    return Column{x.x + r, kvh * G + c - r * G, col < x.z};
+  };
   const bool idle = it.y + wc * 32 >= it.z;  // (the whole wave)
   bf16x8 qf[KS];
   {
-    const bf16* qp = q + (int64_t)row * ld + (int64_t)head * DH + kg * 8;
+    const Column c = column_of(it);
+    const bf16* qp = q + (int64_t)c.row * ld + (int64_t)c.head * DH + kg * 8;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) qf[kk] = ld_bf16x8(qp + kk * 16);
   }
@@ -232,6 +724,9 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
   auto request = [&](unsigned lds_addr, const bf16* from) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(from) : "memory");
   };
+  auto request_from = [&](unsigned lds_addr, const bf16* base, unsigned bytes) {  // base: the same for the wave
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(bytes), "s"(base) : "memory");
+  };
   auto load_block = [&](int buf) {
     if constexpr (KV8) {
 #pragma unroll
@@ -248,11 +743,11 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
 #pragma unroll
       for (int p = 0; p < KP; ++p) {
         const int pg = w * KP + p;  // of the block
-        const bf16* kp = (const bf16*)kv.k_pool + ((int64_t)k_page[p] * Hkv + kvh) * HEAD;
+        const bf16* kp = (const bf16*)kv.k_pool + ((int64_t)__builtin_amdgcn_readfirstlane(k_page[p]) * Hkv + kvh) * HEAD;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
           const int slot = j * TPI + lane / CR, ktok = (pg & 1) * 16 + slot, kc = (lane % CR) ^ ((ktok / RWK) % CR);
-          request(k_lds + ((buf * NH + (pg >> 1)) * HALF + ((pg & 1) * 16 + j * TPI) * DH) * 2, kp + (kc / 4) * 512 + slot * 32 + kc % 4 * 8);
+          request_from(k_lds + ((buf * NH + (pg >> 1)) * HALF + ((pg & 1) * 16 + j * TPI) * DH) * 2, kp, ((kc / 4) * 512 + slot * 32 + kc % 4 * 8) * 2);
         }
       }
       const int half = w / WPH, part = w % WPH;
@@ -403,8 +898,13 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
         }
     }
   }
-  if (!real) return;
-  const int64_t slot = ((int64_t)row * n_q_heads + head) * max_spans + it.w;
+  // (the item is read again: what it says would hold registers through all of the above)
+  int item_again = item;
+  asm volatile("" : "+s"(item_again));
+  const int4 again = items[2 * item_again];
+  const Column c = column_of(again);
+  if (!c.real) return;
+  const int64_t slot = ((int64_t)c.row * n_q_heads + c.head) * max_spans + again.w;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -416,48 +916,69 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
 
 }  // namespace
 
-int attn_prefix_items(int batch, int n_groups, int n_q_heads, int n_kv_heads) {
-  const int G = n_q_heads / n_kv_heads;
-  return (int)(((int64_t)batch * G) / tile_columns(batch, n_groups, G)) + n_groups + spans_wanted(n_kv_heads);
-}
 int attn_prefix_items_most(int max_batch, int n_q_heads, int n_kv_heads) {
-  return max_batch * (n_q_heads / n_kv_heads) / 32 + max_batch + spans_wanted(n_kv_heads);
+  return max_batch * (n_q_heads / n_kv_heads) / 16 + max_batch + (8 * kResident + n_kv_heads - 1) / n_kv_heads;
 }
 
-hipError_t launch_attn_shared_plan(const int32_t* group_starts, int n_groups, const int32_t* lens, int add, const int32_t* block_tables,
-                                   int max_pages_per_seq, int batch, int n_q_heads, int n_kv_heads, const SharedScratch& sc, hipStream_t s) {
-  const SharedRows rows{sc.row_pages, sc.span_pages, add};
-  const int G = n_q_heads / n_kv_heads;
-  shared_prefix_kernel<<<n_groups, 1024, 0, s>>>(group_starts, lens, block_tables, max_pages_per_seq, batch, rows, sc.row_pages, sc.group_pages,
-                                             sc.group_first);
-  shared_list_kernel<<<1, 1024, 0, s>>>(group_starts, n_groups, batch, G, tile_columns(batch, n_groups, G), spans_wanted(n_kv_heads), sc.group_pages,
-                                        sc.group_first, sc.span_pages, sc.items, attn_prefix_items(batch, n_groups, n_q_heads, n_kv_heads));
+// Spans of what rows have behind their prefix: as in decode attention where four waves share one, shorter where each is a wave's.
+int attn_shared_span(int batch, int n_kv_heads) {
+  return rows_split(batch, n_kv_heads) ? attn_decode_span(batch, n_kv_heads) : (int64_t)batch * n_kv_heads >= 4096 ? 1024 : 512;
+}
+
+hipError_t launch_attn_shared_plan(const SharedBatch& b, const SharedScratch& sc, hipStream_t s) {
+  if (b.batch <= 0) return hipSuccess;
+  const Form f = form_of(b.batch, b.n_groups, b.n_q_heads, b.n_kv_heads);
+  const int workgroups = b.n_groups > 0 ? std::min(64, (b.batch + kPlanRows - 1) / kPlanRows) : 1;
+  const PlanArgs a{b, f.columns, f.wanted, items_of(b, f), sc.row_pages, sc.group, sc.done, sc.counts, sc.prefix_items, sc.row_items};
+  shared_plan_kernel<<<workgroups, kPlanThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_attn_prefix(const void* q, int64_t ld, int batch, int n_groups, int n_q_heads, const KvLayout& kv, const SharedScratch& sc,
-                              const int32_t* block_tables, int max_pages_per_seq, float* part_o, float* part_ml, int max_spans,
-                              hipStream_t s) {
+hipError_t launch_attn_shared(const SharedBatch& b, const SharedScratch& sc, const void* q, int64_t ld, const KvLayout& kv, float* part_o,
+                              float* part_ml, unsigned* spans_done, int max_spans, void* out, OperandLayout out_layout, hipStream_t s) {
+  if (b.batch <= 0) return hipSuccess;
   // 8-bit pools hold value / scale: the key scale joins the softmax scale, the value scale the final division, behind the partials
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)kv.head_dim) * (kv.fp8 ? kv.k_scale : 1.0f);
-  const unsigned grid = (unsigned)attn_prefix_items(batch, n_groups, n_q_heads, kv.n_kv_heads) * kv.n_kv_heads;
-  const int columns = tile_columns(batch, n_groups, n_q_heads / kv.n_kv_heads);
+  const float out_scale = kv.fp8 ? kv.v_scale : 1.0f;
+  const Form f = form_of(b.batch, b.n_groups, b.n_q_heads, b.n_kv_heads);
+  const int64_t prefix_units = (int64_t)items_of(b, f) * b.n_kv_heads;
+  const int64_t row_units = (int64_t)b.batch * ((b.max_pages_per_seq * 16 + b.span_len - 1) / b.span_len) * b.n_kv_heads;
+  const bool rows_alone = rows_split(b.batch, b.n_kv_heads);
+  // (workgroups of the sixteen-column kernel take one unit after another)
+  auto grid_of = [](int64_t units, bool split) { return (unsigned)std::min<int64_t>(split ? units : (units + 3) / 4, 8 * kResident); };
+#define TDP_COLUMNS_(DH, KV8, PREFIX, SPLIT, grid, items, count)                                                                         \
+  attn_columns_kernel<DH, KV8, PREFIX, SPLIT><<<grid, 256, 0, s>>>((const bf16*)q, ld, b.n_q_heads, kv, items, count, b.block_tables,    \
+                                                                   b.max_pages_per_seq, part_o, part_ml, spans_done, max_spans, b.span_len, \
+                                                                   (bf16*)out, out_layout, scale_log2, out_scale)
+#define TDP_COLUMNS(DH, KV8, PREFIX, split, units, items, count)                            \
+  do {                                                                                      \
+    const unsigned grid = grid_of(units, split);                                            \
+    if (split) TDP_COLUMNS_(DH, KV8, PREFIX, true, grid, items, count);                     \
+    else TDP_COLUMNS_(DH, KV8, PREFIX, false, grid, items, count);                          \
+  } while (0)
 #define TDP_PREFIX_(DH, NWC, KV8)                                                                                                   \
-  attn_prefix_kernel<DH, NWC, KV8><<<grid, 256, 0, s>>>((const bf16*)q, ld, n_q_heads, kv, sc.items, block_tables, max_pages_per_seq, \
-                                                        part_o, part_ml, max_spans, scale_log2)
-#define TDP_PREFIX(DH, KV8)                          \
-  do {                                               \
-    if (columns == 32) TDP_PREFIX_(DH, 1, KV8);      \
-    else if (columns == 64) TDP_PREFIX_(DH, 2, KV8); \
-    else TDP_PREFIX_(DH, 4, KV8);                    \
+  attn_prefix_kernel<DH, NWC, KV8><<<(unsigned)prefix_units, 256, 0, s>>>((const bf16*)q, ld, b.n_q_heads, kv, sc.prefix_items, sc.counts, \
+                                                                          b.block_tables, b.max_pages_per_seq, part_o, part_ml, max_spans, \
+                                                                          scale_log2)
+#define TDP_SHARED(DH, KV8)                                                                                   \
+  do {                                                                                                        \
+    if (b.n_groups > 0) {                                                                                     \
+      if (f.columns == 16) TDP_COLUMNS(DH, KV8, true, f.split, prefix_units, sc.prefix_items, sc.counts);     \
+      else if (f.columns == 32) TDP_PREFIX_(DH, 1, KV8);                                                      \
+      else if (f.columns == 64) TDP_PREFIX_(DH, 2, KV8);                                                      \
+      else TDP_PREFIX_(DH, 4, KV8);                                                                           \
+    }                                                                                                         \
+    TDP_COLUMNS(DH, KV8, false, rows_alone, row_units, sc.row_items, sc.counts + 1);                        \
   } while (0)
   if (kv.head_dim == 128) {
-    if (kv.fp8) TDP_PREFIX(128, true); else TDP_PREFIX(128, false);
+    if (kv.fp8) TDP_SHARED(128, true); else TDP_SHARED(128, false);
   } else {
-    if (kv.fp8) TDP_PREFIX(64, true); else TDP_PREFIX(64, false);
+    if (kv.fp8) TDP_SHARED(64, true); else TDP_SHARED(64, false);
   }
-#undef TDP_PREFIX
+#undef TDP_SHARED
 #undef TDP_PREFIX_
+#undef TDP_COLUMNS
+#undef TDP_COLUMNS_
   return hipGetLastError();
 }
 

@@ -172,30 +172,11 @@ struct Groups {
   int n;
 };
 
-// Plan and kernels of attention over groups, in the first scratch set; rows attend to lens + add tokens.
-hipError_t plan_shared(tdp_stage* st, const Groups& groups, const int32_t* lens, int add, const int32_t* block_tables, int batch, int span_len,
-                       hipStream_t s) {
+// A decode batch (or the rows of tdp_stage_attend) with its groups, as the kernels for shared prefixes want it.
+SharedBatch shared_batch(const tdp_stage* st, const Groups& groups, const int32_t* lens, int add, const int32_t* block_tables, int batch) {
   const tdp_stage_config& c = st->cfg;
-  tdp_stage::Scratch& sc = st->sc[0];
-  if (groups.n > 0) {
-    const hipError_t e = launch_attn_shared_plan(groups.starts, groups.n, lens, add, block_tables, c.max_pages_per_seq, batch, c.n_q_heads,
-                                                 c.n_kv_heads, sc.shared, s);
-    if (e != hipSuccess) return e;
-  }
-  const SharedRows rows{groups.n > 0 ? sc.shared.row_pages : nullptr, sc.shared.span_pages, add};
-  return launch_attn_plan(lens, block_tables, c.max_pages_per_seq, batch, st->max_chunks, span_len, sc.attn_items, sc.attn_item_pages, s, &rows);
-}
-hipError_t attend_shared(tdp_stage* st, const Groups& groups, const void* q, int64_t ld, const KvLayout& kv, const int32_t* block_tables, int batch,
-                         int span_len, void* out, const OperandLayout& out_layout, hipStream_t s) {
-  const tdp_stage_config& c = st->cfg;
-  tdp_stage::Scratch& sc = st->sc[0];
-  if (groups.n > 0) {
-    const hipError_t e = launch_attn_prefix(q, ld, batch, groups.n, c.n_q_heads, kv, sc.shared, block_tables, c.max_pages_per_seq, sc.part_o, sc.part_ml,
-                                            st->max_chunks, s);
-    if (e != hipSuccess) return e;
-  }
-  return launch_attn_decode(DecodeQueries{q, ld, nullptr, nullptr, nullptr, 1}, batch, c.n_q_heads, kv, sc.attn_items, sc.attn_item_pages, span_len / 16,
-                            nullptr, sc.part_o, sc.part_ml, sc.spans_done, st->max_chunks, span_len, out, out_layout, s, true);
+  const int span = st->decode_span > 0 ? st->decode_span : attn_shared_span(batch, c.n_kv_heads);
+  return {groups.n > 0 ? groups.starts : nullptr, groups.n, lens, block_tables, add, batch, c.max_pages_per_seq, c.n_q_heads, c.n_kv_heads, span};
 }
 
 // The layer sequence shared by both phases.  M tokens; decode when ctx_lens != null, with groups if some are given.
@@ -212,7 +193,8 @@ int run_layers(tdp_stage* st, tdp_stage::Scratch& sc, bool timed, const void* hi
   int x_f32 = 0;
   const int span_len = st->decode_span > 0 ? st->decode_span : attn_decode_span(M, c.n_kv_heads);
   const bool planned = ctx_lens && !groups && attn_decode_planned(M, c.n_kv_heads, st->max_chunks, span_len);
-  if (groups) HIP_TRY(plan_shared(st, *groups, ctx_lens, 1, block_tables, M, span_len, s));
+  const SharedBatch shared = groups ? shared_batch(st, *groups, ctx_lens, 1, block_tables, M) : SharedBatch{};
+  if (groups) HIP_TRY(launch_attn_shared_plan(shared, sc.shared, s));
   if (planned)
     HIP_TRY(launch_attn_plan(ctx_lens, block_tables, c.max_pages_per_seq, M, st->max_chunks, span_len, sc.attn_items,
                              sc.attn_item_pages, s));
@@ -282,7 +264,8 @@ int run_layers(tdp_stage* st, tdp_stage::Scratch& sc, bool timed, const void* hi
     {  // a4: attention
       Timer t(st, s, timed, T_ATTN);
       if (groups)
-        HIP_TRY(attend_shared(st, *groups, sc.qkv, st->Nqkv_pad, kv, block_tables, M, span_len, sc.attn, layout_paired(st->dq), s));
+        HIP_TRY(launch_attn_shared(shared, sc.shared, sc.qkv, st->Nqkv_pad, kv, sc.part_o, sc.part_ml, sc.spans_done, st->max_chunks, sc.attn,
+                                   layout_paired(st->dq), s));
       else if (ctx_lens)
         HIP_TRY(launch_attn_decode(dq, M, c.n_q_heads, kv, planned ? sc.attn_items : nullptr,
                                    planned ? sc.attn_item_pages : block_tables,
@@ -417,12 +400,13 @@ int tdp_stage_create(const tdp_stage_config* cfg, tdp_stage** out) {
     A(&sc.attn_items, mb * st->max_chunks, false);
     if (i == 0) {
       A(&sc.token_pages, c.max_tokens, false);
-      A(&sc.shared.row_pages, mb, true);
-      A(&sc.shared.group_pages, mb, true);
-      A(&sc.shared.group_first, mb, true);
-      A(&sc.shared.span_pages, 1, true);
-      A(&sc.shared.items, 2 * (int64_t)attn_prefix_items_most(c.max_batch, c.n_q_heads, c.n_kv_heads), false);
+      A(&sc.shared.row_pages, mb, false);
+      A(&sc.shared.group, 4 * mb, false);
+      A(&sc.shared.done, 1, true);
+      A(&sc.shared.counts, 2, true);
+      A(&sc.shared.prefix_items, 2 * (int64_t)attn_prefix_items_most(c.max_batch, c.n_q_heads, c.n_kv_heads), false);
     }
+    if (i == 0) sc.shared.row_items = sc.attn_items;
     // spans longer than the minimum round the span count up: up to (1024 / 256 - 1) extra minimum spans' worth
     A(&sc.attn_item_pages, mb * (st->max_chunks + kDecodeSpanMax / kDecodeSpanMin) * (kDecodeSpanMin / 16), false);
   }
@@ -464,8 +448,8 @@ void tdp_stage_destroy(tdp_stage* st) {
     if (p) (void)hipFree(p);
   for (tdp_stage::Scratch& sc : st->sc) {
     void* sp[] = {sc.y, sc.qkv, sc.qkv32, sc.attn, sc.h, sc.u, sc.xa, sc.xb, sc.ws, sc.part_o, sc.part_ml,
-                  sc.spans_done, sc.attn_items, sc.attn_item_pages, sc.token_pages, sc.shared.row_pages, sc.shared.group_pages,
-                  sc.shared.group_first, sc.shared.span_pages, sc.shared.items};
+                  sc.spans_done, sc.attn_items, sc.attn_item_pages, sc.token_pages, sc.shared.row_pages, sc.shared.group,
+                  sc.shared.done, sc.shared.counts, sc.shared.prefix_items};
     for (void* p : sp)
       if (p) (void)hipFree(p);
   }
@@ -678,11 +662,12 @@ int tdp_stage_attend(tdp_stage* st, int32_t layer, const void* q, const int32_t*
   if (((uintptr_t)q & 15) || ((uintptr_t)out & 7)) return fail(TDP_EINVAL, "q must be 16-byte and out 8-byte aligned");
   const int rc = check_groups(st, group_starts, n_groups);
   if (rc != TDP_OK) return rc;
-  const Groups groups{group_starts, n_groups};
-  const int span_len = st->decode_span > 0 ? st->decode_span : attn_decode_span(batch, st->cfg.n_kv_heads);
+  const SharedBatch shared = shared_batch(st, Groups{group_starts, n_groups}, lens, 0, block_tables, batch);
+  const tdp_stage::Scratch& sc = st->sc[0];
   hipStream_t s = (hipStream_t)stream;
-  HIP_TRY(plan_shared(st, groups, lens, 0, block_tables, batch, span_len, s));
-  HIP_TRY(attend_shared(st, groups, q, st->dq, kv_layout(st, layer), block_tables, batch, span_len, out, layout_row_major(st->dq), s));
+  HIP_TRY(launch_attn_shared_plan(shared, sc.shared, s));
+  HIP_TRY(launch_attn_shared(shared, sc.shared, q, st->dq, kv_layout(st, layer), sc.part_o, sc.part_ml, sc.spans_done, st->max_chunks, out,
+                             layout_row_major(st->dq), s));
   return TDP_OK;
 }
 

@@ -67,6 +67,17 @@ __device__ __forceinline__ int decode_position(int ctx, int max_pages_per_seq) {
   return min(max(ctx, 0), max_pages_per_seq * 16 - 1);
 }
 
+// Numbers past the caches of an XCD, for workgroups of other XCDs in the same launch.
+__device__ __forceinline__ void store_agent(float* p, float v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_agent2(const float* p) {  // (8-byte aligned)
+  return __builtin_bit_cast(float2, __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ __forceinline__ void store_agent(int32_t* p, int32_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ int32_t load_agent(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
 // Softmax in the exp2 domain: a finite stand-in for -inf (exp2 gives exactly 0, no inf - inf), and by how much (log2 units) a block may
 // exceed the reference before sums are rescaled.
 constexpr float kNegBig = -1.0e30f;

@@ -269,28 +269,8 @@ int attn_decode_span(int batch, int n_kv_heads);
 // its unused tail marked with request -1 up to attn_decode_items(), and per item the physical pages
 // of its span (span_len / 16 entries each)
 int attn_decode_items(int batch, int max_spans, int span_len);
-// What rows of a batch share (launch_attn_shared_plan): `pages` pages of row b at the front of it, read once for its group in spans of
-// *span_pages pages or more.
-struct SharedRows {
-  const int32_t *row_pages, *span_pages;  // null: nothing
-  int add;                                // tokens of a row beyond its length: 1 in a decode step
-#ifdef __HIPCC__
-  __device__ __forceinline__ int tokens(int len, int max_pages_per_seq) const {
-    return min(max(len, 0) + add, max_pages_per_seq * 16);
-  }
-  // Whole pages in front of the row's last token.  Fewer than the shortest span of them only where the row has one span behind them (so
-  // the plan makes them): the partials of the prefix's spans and of the row's own are no more than those of spans of its whole length.
-  __device__ __forceinline__ int prefix(int b, int len, int max_pages_per_seq) const {
-    if (!row_pages) return 0;
-    const int n = tokens(len, max_pages_per_seq), pages = max(0, min(row_pages[b], (n - 1) >> 4));
-    return pages * 16 < kDecodeSpanMin && n - pages * 16 > kDecodeSpanMin ? 0 : pages;
-  }
-  __device__ __forceinline__ int spans(int pages) const { return pages > 0 ? max(1, pages / *span_pages) : 0; }
-#endif
-};
 hipError_t launch_attn_plan(const int32_t* ctx_lens, const int32_t* block_tables, int max_pages_per_seq, int batch,
-                            int max_spans, int span_len, int4* items, int32_t* item_pages, hipStream_t s,
-                            const SharedRows* shared = nullptr);
+                            int max_spans, int span_len, int4* items, int32_t* item_pages, hipStream_t s);
 // The attention kernel: finishes every request whose context fits one span in one workgroup per K/V head; of a longer one
 // the workgroups leave fp32 partials (part_o, part_ml).  With spans_done [batch][n_kv_heads] (zero before the first launch, zero
 // again after every launch) they count the finished spans, and the last of them to finish combines them; with null,
@@ -313,23 +293,31 @@ bool attn_decode_planned(int batch, int n_kv_heads, int max_spans, int span_len)
 hipError_t launch_attn_decode(const DecodeQueries& dq, int batch, int n_q_heads, const KvLayout& kv,
                               const int4* items, const int32_t* item_pages, int item_pitch, const int32_t* ctx_lens,
                               float* part_o, float* part_ml, unsigned* spans_done, int max_spans, int span_len,
-                              void* out, OperandLayout out_layout, hipStream_t s, bool shared = false);
-// Attention over prefixes that the rows of a group share, once for all (query head, row) columns of the group.  group_starts dev
-// int32 [n_groups + 1].  The plan (once per step): how many leading pages all rows of a group agree on, and the work list; then,
-// for every layer, the prefix kernel, which leaves partials in the first slots of every row and head, and the decode kernel on
-// what is behind (launch_attn_plan and launch_attn_decode with `shared`), which always counts spans.
+                              void* out, OperandLayout out_layout, hipStream_t s);
+// Attention of rows that may share prefixes: what the plan (once per step) finds the rows of a group to share is attended to once for all
+// of the group's (query head, row) columns, and what a row has behind that by the row itself.  group_starts dev int32 [n_groups + 1].
 struct SharedScratch {
-  int32_t *row_pages, *group_pages, *group_first;  // [max_batch] each
-  int32_t* span_pages;                             // [1]
-  int4* items;                                     // two for each
+  int32_t* row_pages;  // [max_batch]
+  int32_t* group;      // [4 * max_batch]
+  unsigned* done;      // [1]: workgroups of the plan that are through; zero between launches
+  int32_t* counts;     // [2]: items of the two lists
+  int4* prefix_items;  // two records each
+  int4* row_items;     // [max_batch * max_spans]
 };
-int attn_prefix_items(int batch, int n_groups, int n_q_heads, int n_kv_heads);  // of the list at most
-int attn_prefix_items_most(int max_batch, int n_q_heads, int n_kv_heads);       // whatever the batch and its groups
-hipError_t launch_attn_shared_plan(const int32_t* group_starts, int n_groups, const int32_t* lens, int add, const int32_t* block_tables,
-                                   int max_pages_per_seq, int batch, int n_q_heads, int n_kv_heads, const SharedScratch& sc, hipStream_t s);
-hipError_t launch_attn_prefix(const void* q, int64_t ld, int batch, int n_groups, int n_q_heads, const KvLayout& kv, const SharedScratch& sc,
-                              const int32_t* block_tables, int max_pages_per_seq, float* part_o, float* part_ml, int max_spans,
-                              hipStream_t s);
+int attn_prefix_items_most(int max_batch, int n_q_heads, int n_kv_heads);  // of the prefix list, whatever the batch and its groups
+// Rows attend to lens[b] + add tokens (0 .. 16 * max_pages_per_seq); a row's tokens behind the prefix are cut into spans of span_len.
+struct SharedBatch {
+  const int32_t* group_starts;  // null with n_groups = 0
+  int n_groups;
+  const int32_t *lens, *block_tables;
+  int add, batch, max_pages_per_seq, n_q_heads, n_kv_heads, span_len;
+};
+int attn_shared_span(int batch, int n_kv_heads);
+hipError_t launch_attn_shared_plan(const SharedBatch& b, const SharedScratch& sc, hipStream_t s);
+// Both kernels of a layer: partials of the prefix in the first slots of every row and head, then the rows, which combine them with their
+// own.  spans_done as in launch_attn_decode.
+hipError_t launch_attn_shared(const SharedBatch& b, const SharedScratch& sc, const void* q, int64_t ld, const KvLayout& kv, float* part_o,
+                              float* part_ml, unsigned* spans_done, int max_spans, void* out, OperandLayout out_layout, hipStream_t s);
 hipError_t launch_attn_decode_merge(int batch, int n_q_heads, const KvLayout& kv, const int32_t* ctx_lens,
                                     int max_pages_per_seq, const float* part_o, const float* part_ml, int max_spans,
                                     int span_len, void* out, OperandLayout out_layout, hipStream_t s);
