@@ -6,8 +6,10 @@
 // candidates of all beams.
 //
 // Scores of different beams are often close, and which token goes on depends on their order, so what is compared is in 64 bits.  The
-// exponentials are in fp32: e^d as 2^(d log2 e), the product in two parts, so that all of it but the instruction's own error (1 ulp, in no
-// order) and the sums of a thread's terms is exact to 2^-24 of a term.  Over thousands of terms that averages out to below 1e-8 of the sum.
+// exponentials are in fp32, e^(z - r) = 2^(z log2 e - R) for an R near r log2 e: log2 e in two parts, a fused multiply-add each, so that the
+// exponent is rounded by 2^-24 of itself and nothing large cancels; what is summed is relative to R itself, and the logarithm joins it
+// again in 64 bits.  What is left, the instruction's own error (1 ulp, in no order) and the rounding of a thread's sum, averages out to
+// below 1e-8 of a sum of thousands of terms.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -42,6 +44,7 @@ struct BeamArgs {
   const float* scores;
   // per (row, piece)
   float* max;
+  double* reference;  // R ln 2
   double* sum;
   u64* keys;  // [k], in order, 0 behind the last
   int32_t *parent, *token;
@@ -49,10 +52,10 @@ struct BeamArgs {
   int32_t* finished_out;
 };
 
-// e^d for d <= 0
-__device__ __forceinline__ float exp_close(float d) {
-  constexpr float kHigh = 1.44269502f, kLow = 1.92596299e-8f;  // log2 e
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(d, kHigh, fmaxf(d, -1e30f) * kLow));
+constexpr float kLog2High = 1.44269502f, kLog2Low = 1.92596299e-8f;  // log2 e
+// 2^(z log2 e - R)
+__device__ __forceinline__ float exp_from(float z, float R) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2Low, __builtin_fmaf(z, kLog2High, -R)));
 }
 
 // A piece of a row in vectors from its first element on, wherever that lies in memory: which terms a thread adds up, and with them
@@ -95,6 +98,7 @@ __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restric
     for (int i = tid; i < a.k; i += threads) keys[i] = piece == 0 && i == 0 ? key_of(0.f, a.end_token) : 0;
     if (tid == 0) {
       a.max[slot] = piece == 0 ? 0.f : -INFINITY;
+      a.reference[slot] = 0.0;
       a.sum[slot] = piece == 0 ? 1.0 : 0.0;
     }
     return;
@@ -149,17 +153,24 @@ __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restric
   __syncthreads();
   float max = rs.wave_max[0];
   for (int w = 1; w < waves; ++w) max = fmaxf(max, rs.wave_max[w]);
-  // sums relative to it: a few terms in fp32, the rest in 64 bits
-  const float r = reference_of(max);
-  double total = edge_at >= 0 ? (double)exp_close(edge - r) : 0.0;
+  // Sums relative to it (to 0 where nothing is above minus infinity): a few terms in fp32, the rest in 64 bits.  Logits whose multiple of
+  // log2 e could overflow are taken relative to the maximum first.
+  const float r = max == -INFINITY ? 0.f : max, shift_by = fabsf(r) > 1e37f ? r : 0.f;
+  const float R = (r - shift_by) * kLog2High;
+  double total = edge_at >= 0 ? (double)exp_from(edge - shift_by, R) : 0.0;
   auto add = [&](int v0) {
     float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       if (u > 0 && v0 - tid + u * threads >= row.body) break;  // (the same for all threads)
       asm volatile("" : "+v"(z[u]));  // (bf16: converted here again, the values of two passes would not fit)
+      if (shift_by == 0.f) {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) sum += exp_close(Values::value(z[u], e) - r);
+        for (int e = 0; e < kPer; ++e) sum += exp_from(Values::value(z[u], e), R);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) sum += exp_from(Values::value(z[u], e) - shift_by, R);
+      }
     }
     total += (double)sum;
   };
@@ -178,6 +189,7 @@ __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restric
   if (tid == 0) {
     for (int w = 1; w < waves; ++w) total += wave_total[w];
     a.max[slot] = max;
+    a.reference[slot] = (double)shift_by + (double)R * 0.69314718055994530942;
     a.sum[slot] = total;
   }
   const int found = select_top(
@@ -217,73 +229,103 @@ __device__ __forceinline__ double score_of(u64 order) {
   return __longlong_as_double((long long)(order ^ (order >> 63 ? 1ull << 63 : ~0ull)));
 }
 
-// One workgroup per group.  `lists` = beams * pieces lists of k candidates, each in order.  The first `heads` of every list, n_out in all or
-// more, give a bound: the n_out-th best of them.  A list goes on behind its heads only if all of them reach the bound, so at
-// most n_out / heads lists do, and n_out * k / heads <= 1024 candidates reach it: one to a thread, a few dozen as a rule.
-__global__ __launch_bounds__(1024) void beams_group_kernel(const BeamArgs a) {
+// One workgroup per group, of 256 threads (64 candidates at most) or 1024.  `lists` = beams * pieces lists of k candidates, each in order.  Up to kAllRanked of them are
+// all ranked at once.  Otherwise the first `heads` of every list, n_out in all or more, give a bound, the n_out-th best of them: a
+// list goes on behind its heads only if all of them reach it, so at most n_out / heads lists do, and n_out * k / heads <= 1024 candidates reach
+// it, a few dozen as a rule.
+// Bound: look-ups that wait for each other (three) and barriers.
+constexpr int kAllRanked = 256;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void beams_group_kernel(const BeamArgs a) {
   __shared__ double log_total[TDP_MAX_BEAMS];
   __shared__ Candidate pool[kListsMost];
   __shared__ Candidate bound;
-  __shared__ int count;
+  __shared__ int count, places[kListsMost];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = blockIdx.x;
   const int64_t slot0 = (int64_t)g * a.beams * a.pieces;
-  for (int b = wave; b < a.beams; b += 16) {
+  const int lists = a.beams * a.pieces, all = lists * a.k, n_out = a.k;
+  const u64 own_key = tid < all ? a.keys[slot0 * a.k + tid] : 0;  // (asked for with the sums)
+  const float own_score = tid < all ? a.scores[(int64_t)g * a.beams + tid / (a.pieces * a.k)] : 0.f;
+  for (int b = wave; b < a.beams; b += THREADS / 64) {
     const bool in = lane < a.pieces;
     const int64_t slot = slot0 + b * a.pieces + lane;
     const float own = in ? a.max[slot] : -INFINITY;
+    const double at = in ? a.reference[slot] : 0.0, sum = in ? a.sum[slot] : 0.0;
+    // relative to the reference of the piece with the largest logit
     float max = own;
     for (int o = 1; o < 64; o *= 2) max = fmaxf(max, __shfl_xor(max, o, 64));
-    const double part = in ? a.sum[slot] * exp((double)own - (double)max) : 0.0;  // (nothing but minus infinity: NaN)
-    const double total = wave_sum_double(part);
-    if (lane == 0) log_total[b] = (double)max + log(total);
+    const int of = __ffsll((long long)__ballot(own == max)) - 1;
+    const double reference = __shfl(at, of, 64);
+    // (of a piece with nothing but minus infinity and NaN the sum alone counts: 0, or NaN)
+    const double total = wave_sum_double(own == -INFINITY ? sum : sum * exp(at - reference));
+    if (lane == 0) log_total[b] = max == -INFINITY ? NAN : reference + log(total);
   }
   if (tid == 0) {
     bound = Candidate{0, 0};
     count = 0;
   }
+  for (int i = tid; i < kListsMost; i += THREADS) places[i] = 0;
   __syncthreads();
-  const int lists = a.beams * a.pieces, heads = (a.k + lists - 1) / lists, some = lists * heads;
-  auto candidate = [&](int list, int pos) {
-    const u64 key = a.keys[(slot0 + list) * a.k + pos];
+  auto candidate = [&](u64 key, float score, int beam) {
     if (!key) return Candidate{0, 0};
-    const int beam = list / a.pieces;
     const unsigned order = (unsigned)(key >> 32);
-    const double c = (double)a.scores[(int64_t)g * a.beams + beam] + ((double)logit_of(order) - log_total[beam]);
+    const double c = (double)score + ((double)logit_of(order) - log_total[beam]);
     if (!(c > -INFINITY)) return Candidate{0, 0};
     const long long bits = __double_as_longlong(c + 0.0);
     return Candidate{(u64)bits ^ (bits < 0 ? ~0ull : 1ull << 63),
                      (u64)(31 - beam) << 59 | (u64)order << kIndexBits | ((unsigned)key & ((1u << kIndexBits) - 1))};
   };
-  auto rank = [&](const Candidate& c, int n) {
-    int r = 0;
-    for (int i = 0; i < n; ++i) r += better(pool[i], c);
-    return r;
-  };
-  Candidate own{0, 0};
-  if (tid < some) pool[tid] = own = candidate(tid / heads, tid % heads);
-  __syncthreads();
-  if (own.score && rank(own, some) == a.k - 1) bound = own;  // (no two are equal)
-  __syncthreads();
-  const Candidate least = bound;
-  for (int i = tid; i < lists * a.k; i += 1024) {
-    const Candidate c = candidate(i / a.k, i % a.k);
-    if (c.score && !better(least, c)) pool[atomicAdd(&count, 1)] = c;
-  }
-  __syncthreads();
-  const int n = count, n_out = a.k;
-  if (tid < n) {
-    own = pool[tid];
-    const int place = rank(own, n);
-    if (place < n_out) {
-      const int64_t at = (int64_t)g * n_out + place;
-      const int token = (int)(~own.rest & ((1u << kIndexBits) - 1));
-      a.parent[at] = g * a.beams + 31 - (int)(own.rest >> 59);
-      a.token[at] = token;
-      a.score[at] = (float)score_of(own.score);
-      if (a.finished_out) a.finished_out[at] = token == a.end_token;
+  auto candidate_at = [&](int i) { return candidate(a.keys[slot0 * a.k + i], a.scores[(int64_t)g * a.beams + i / (a.pieces * a.k)], i / (a.pieces * a.k)); };
+  // places[i] = how many of the pool's n are better than its i-th: all pairs, shared out over the threads; behind a barrier on both sides
+  auto rank_all = [&](int n) {
+    int shift = 6;
+    while ((1 << shift) < n) ++shift;
+    const int i = tid & ((1 << shift) - 1), parts = THREADS >> shift;
+    if (i < n) {
+      const Candidate c = pool[i];
+      int r = 0;
+#pragma unroll 4
+      for (int j = tid >> shift; j < n; j += parts) r += better(pool[j], c);
+      if (r) atomicAdd(&places[i], r);
     }
+    __syncthreads();
+  };
+  const Candidate own = candidate(own_key, own_score, tid / (a.pieces * a.k));
+  int n = all, found;  // candidates in the pool, and those among them that are some
+  if (all <= kAllRanked) {
+    if (tid < all) pool[tid] = own;
+    found = __syncthreads_count(own.score != 0);
+  } else {
+    const int heads = (a.k + lists - 1) / lists, some = lists * heads;
+    for (int i = tid; i < some; i += THREADS) pool[i] = candidate_at(i / heads * a.k + i % heads);
+    __syncthreads();
+    rank_all(some);
+    for (int i = tid; i < some; i += THREADS) {
+      if (pool[i].score && places[i] == a.k - 1) bound = pool[i];  // (no two are equal)
+      places[i] = 0;
+    }
+    __syncthreads();
+    const Candidate least = bound;
+    for (int i = tid; i < all; i += THREADS) {
+      const Candidate c = i == tid ? own : candidate_at(i);
+      if (c.score && !better(least, c)) pool[atomicAdd(&count, 1)] = c;
+    }
+    __syncthreads();
+    n = found = count;
   }
-  for (int i = n + tid; i < n_out; i += 1024) {
+  rank_all(n);
+  for (int i = tid; i < n; i += THREADS) {
+    const Candidate c = pool[i];
+    const int place = places[i];
+    if (!c.score || place >= n_out) continue;
+    const int64_t at = (int64_t)g * n_out + place;
+    const int token = (int)(~c.rest & ((1u << kIndexBits) - 1));
+    a.parent[at] = g * a.beams + 31 - (int)(c.rest >> 59);
+    a.token[at] = token;
+    a.score[at] = (float)score_of(c.score);
+    if (a.finished_out) a.finished_out[at] = token == a.end_token;
+  }
+  for (int i = found + tid; i < n_out; i += THREADS) {
     const int64_t at = (int64_t)g * n_out + i;
     a.parent[at] = a.token[at] = -1;
     a.score[at] = -INFINITY;
@@ -297,13 +339,25 @@ int fail_hip(hipError_t e, const char* what) {
   return probe_fail(e == hipErrorOutOfMemory ? TDP_ENOMEM : TDP_EHIP, buf);
 }
 
-// Pieces of a row.  Enough of them that a few rows keep the chip busy, no smaller than a few KiB; a row of many in pieces that the
-// registers of a workgroup hold, as long as they are not too many.
-int pieces_of(int rows, int n, int per) {
-  const int full = (n + per * kInFlight * 1024 - 1) / (per * kInFlight * 1024);
-  const int wanted = std::min({kPiecesMost, kListsMost / 2 / rows, n / (per * 1024)});
-  return std::max(1, std::max(std::min(full, kPiecesOfMany), wanted));
+// How a row is cut.  A few rows into enough pieces that they keep the chip busy, of some thousand logits at least (the second kernel ranks
+// candidates of every piece: 2 rows of 5 beams, 128256 logits, 31 / 25 pieces 14.8 / 12.3 us).  Many into pieces that the registers of a
+// workgroup of 1024 threads hold, as long as they are not too many; bf16, twice as many logits to a thread, of 512 (528 rows of 152067, 3
+// pieces 56 us, 5 of half the threads 49; fp32 70 and 83).
+struct Cut {
+  int pieces, threads;
+};
+Cut cut_of(int rows, int n, int per) {
+  const int most = per == 4 ? 1024 : 512;
+  const int full = (n + per * kInFlight * most - 1) / (per * kInFlight * most);
+  const int wanted = std::min({kPiecesMost, kListsMost / 4 / rows, n / (per * 1024)});
+  const int pieces = std::max(1, std::max(std::min(full, kPiecesOfMany), wanted));
+  const int vectors = ((n + pieces - 1) / pieces + per - 1) / per;
+  int threads = 64;  // four vectors to a thread, eight at most if 1024 are enough for that
+  while (threads < 1024 && threads * (threads < most ? 4 : kInFlight) < vectors) threads *= 2;
+  return {pieces, threads};
 }
+
+size_t slots_of(int max_rows) { return std::max<size_t>(kListsMost, (size_t)kPiecesOfMany * max_rows); }
 
 }  // namespace
 }  // namespace tdp
@@ -314,7 +368,7 @@ struct tdp_beams {
   tdp_beams_config cfg;
   int device = 0;
   float* max = nullptr;
-  double* sum = nullptr;
+  double* sum = nullptr;  // and the references behind them
   u64* keys = nullptr;
 };
 
@@ -330,9 +384,9 @@ int tdp_beams_create(const tdp_beams_config* cfg, tdp_beams** out) {
   if (!h) return probe_fail(TDP_ENOMEM, "host allocation failed");
   h->cfg = *cfg;
   h->device = dev;
-  const size_t slots = std::max<size_t>(kListsMost, (size_t)kPiecesOfMany * cfg->max_rows);
+  const size_t slots = slots_of(cfg->max_rows);
   hipError_t e = hipMalloc((void**)&h->max, slots * sizeof(float));
-  if (e == hipSuccess) e = hipMalloc((void**)&h->sum, slots * sizeof(double));
+  if (e == hipSuccess) e = hipMalloc((void**)&h->sum, 2 * slots * sizeof(double));
   if (e == hipSuccess) e = hipMalloc((void**)&h->keys, slots * cfg->max_out * sizeof(u64));
   if (e != hipSuccess) {
     const int code = fail_hip(e, "tdp_beams_create");
@@ -370,14 +424,15 @@ int tdp_beams_select(tdp_beams* h, const void* logits, int32_t dtype, int32_t n_
   if (e != hipSuccess) return fail_hip(e, "hipGetDevice");
   if (dev != h->device) return probe_fail(TDP_EINVAL, "the object was created on another device than the current one");
   hipStream_t s = (hipStream_t)stream;
-  const int rows = n_groups * beams, per = dtype == TDP_F32 ? 4 : 8, pieces = pieces_of(rows, n, per);
-  const int width = ((n + pieces - 1) / pieces + 7) / 8 * 8, used = (n + width - 1) / width, vectors = (std::min(width, n) + per - 1) / per;
-  int threads = 64;  // two vectors to a thread, if 1024 are enough for that
-  while (threads < 1024 && threads * 2 < vectors) threads *= 2;
+  const int rows = n_groups * beams, per = dtype == TDP_F32 ? 4 : 8;
+  const Cut cut = cut_of(rows, n, per);
+  const int width = ((n + cut.pieces - 1) / cut.pieces + 7) / 8 * 8, used = (n + width - 1) / width;
+  const int vectors = (std::min(width, n) + per - 1) / per, threads = cut.threads;
   const bool keep = vectors <= threads * kInFlight;
   int shift = 0;  // of the elements that a thread has read
   while ((1 << shift) < (vectors + threads - 1) / threads * per) ++shift;
-  const BeamArgs a{beams, n, width, used, n_out, finished, end_token, scores, h->max, h->sum, h->keys, parent, token, score, finished_out};
+  const size_t slots = slots_of(h->cfg.max_rows);
+  const BeamArgs a{beams, n, width, used, n_out, finished, end_token, scores, h->max, h->sum + slots, h->sum, h->keys, parent, token, score, finished_out};
   const unsigned grid = (unsigned)rows * used;
   const size_t lds = keep ? threads / 64 * sizeof(StagedUnits) : 0;
 #define TDP_PIECES(T, KEEP) beams_piece_kernel<T, KEEP><<<grid, threads, lds, s>>>((const T*)logits, ld, shift, a)
@@ -387,7 +442,8 @@ int tdp_beams_select(tdp_beams* h, const void* logits, int32_t dtype, int32_t n_
     if (keep) TDP_PIECES(bf16, true); else TDP_PIECES(bf16, false);
   }
 #undef TDP_PIECES
-  beams_group_kernel<<<n_groups, 1024, 0, s>>>(a);
+  if (beams * used * n_out <= 64) beams_group_kernel<256><<<n_groups, 256, 0, s>>>(a);
+  else beams_group_kernel<1024><<<n_groups, 1024, 0, s>>>(a);
   e = hipGetLastError();
   return e == hipSuccess ? TDP_OK : fail_hip(e, "tdp_beams_select");
 }
