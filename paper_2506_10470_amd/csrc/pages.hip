@@ -265,19 +265,11 @@ struct CompactArgs {
   // scratch
   u64 *free_marks, *movable_marks;
   int *free_counts, *movable_counts, *used_counts;
-  int* named;      // [num_pages] entries of the rows that name a page; then the id that it has behind the call
+  int* named;      // [num_pages] entries of the rows that name a page; zero between calls
+  int* moved;      // [num_pages] the id that it has behind the call
   int *from, *to;  // [num_pages] the k-th highest movable page, the k-th lowest free one
-  int* totals;     // refused rows
+  int* totals;     // refused rows; zero between calls
 };
-
-__global__ __launch_bounds__(256) void compact_clear_kernel(const CompactArgs a) {
-  const int p = blockIdx.x * 256 + threadIdx.x;
-  if (p == 0) a.totals[0] = 0;
-  if (p < a.num_pages) {
-    a.named[p] = 0;
-    if (a.refs_out != a.refs_in) a.refs_out[p] = a.refs_in[p];
-  }
-}
 
 __global__ __launch_bounds__(256) void compact_count_kernel(const CompactArgs a) {
   const int r = blockIdx.x, len = a.lens[r];
@@ -299,8 +291,12 @@ __global__ __launch_bounds__(1024) void compact_survey_kernel(const CompactArgs 
   for (int i = 0; i < kChunkWords / 16; ++i) {
     const int w = wave * (kChunkWords / 16) + i, p = c * kChunk + w * 64 + lane;
     const bool in = p < a.num_pages;
-    const int refs = in ? a.refs_out[p] : -1, named = in ? a.named[p] : 0;
-    if (in) a.named[p] = p;
+    const int refs = in ? a.refs_in[p] : -1, named = in ? a.named[p] : 0;
+    if (in) {
+      a.named[p] = 0;
+      a.moved[p] = p;
+      if (a.refs_out != a.refs_in) a.refs_out[p] = refs;
+    }
     const u64 free = __ballot(refs == 0), movable = __ballot(refs > 0 && refs == named);
     found[0] += __popcll(free);
     found[1] += __popcll(movable);
@@ -353,24 +349,28 @@ __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a) 
   a.moves[2 * (int64_t)k + 1] = goes ? a.to[k] : -1;
   if (!goes) return;
   const int from = a.from[k], to = a.to[k];
-  a.named[from] = to;
+  a.moved[from] = to;
   a.refs_out[to] = a.refs_out[from];
   a.refs_out[from] = 0;
 }
 
 __global__ __launch_bounds__(256) void compact_tables_kernel(const CompactArgs a) {
   const int r = blockIdx.x;
+  if (r == 0 && threadIdx.x == 0) a.totals[0] = 0;
   const int held = pages_of(min(max(a.lens[r], 0), a.width * kPage));
   for (int e = threadIdx.x; e < a.width; e += 256) {
     const int64_t at = (int64_t)r * a.width + e;
     const int page = e < held ? a.src_tables[at] : -1;
-    a.dst_tables[at] = page >= 0 && page < a.num_pages ? a.named[page] : page;
+    a.dst_tables[at] = page >= 0 && page < a.num_pages ? a.moved[page] : page;
   }
 }
 
 // ---- page contents ---------------------------------------------------------------------------------------------------------------
 
-// A workgroup copies up to 16 KiB of one page of one pool of one layer.
+// A workgroup copies up to 16 KiB of one page of one pool of one layer.  Bound: HBM, 5.4 TB/s read and written (268 MB, 50 us).  The stores are
+// non-temporal: what they would displace in the caches is worth more to the decode step behind than the pages themselves (copies of 26 MB,
+// and with two layers of attention over 64 x 8 rows behind them that reads them: ordinary 19 and 303 us, so 7 and 289, the loads as well
+// 10 and 289; of 105 MB and eight layers 40 and 1173, 26 and 1153, 40 and 1149).
 constexpr int kCopyBytes = 16384;
 __global__ __launch_bounds__(256) void pages_copy_kernel(uint8_t* k_pool, uint8_t* v_pool, int64_t layer_bytes, int64_t page_bytes,
                                                          int num_pages, const int32_t* __restrict__ pairs, int pieces) {
@@ -388,7 +388,8 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(uint8_t* k_pool, uint8_
     if ((int)threadIdx.x + 256 * j < n) v[j] = src[threadIdx.x + 256 * j];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if ((int)threadIdx.x + 256 * j < n) dst[threadIdx.x + 256 * j] = v[j];
+    if ((int)threadIdx.x + 256 * j < n)
+      __builtin_nontemporal_store(__builtin_bit_cast(i32x4, v[j]), reinterpret_cast<i32x4*>(dst) + threadIdx.x + 256 * j);
 }
 
 int fail_hip(hipError_t e, const char* what) {
@@ -445,11 +446,13 @@ int tdp_pages_create(const tdp_pages_config* cfg, tdp_pages** out) {
   h->cfg = *cfg;
   h->device = dev;
   h->chunks = (cfg->num_pages + kChunk - 1) / kChunk;
+  const size_t ints = ((size_t)3 * h->chunks + 3 + 3 * (size_t)cfg->max_rows + 4 * (size_t)cfg->num_pages) * sizeof(int);
   hipError_t e = hipMalloc((void**)&h->marks, (size_t)2 * h->chunks * kChunkWords * sizeof(u64));
-  if (e == hipSuccess)
-    e = hipMalloc((void**)&h->ints, ((size_t)3 * h->chunks + 2 + 3 * (size_t)cfg->max_rows + 3 * (size_t)cfg->num_pages) * sizeof(int));
+  if (e == hipSuccess) e = hipMalloc((void**)&h->ints, ints);
+  if (e == hipSuccess) e = hipMemset(h->ints, 0, ints);
   if (e == hipSuccess)
     e = hipFuncSetAttribute((const void*)pages_survey_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kRowsMost * (int)sizeof(int));
+  if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     const int code = fail_hip(e, "tdp_pages_create");
     tdp_pages_destroy(h);
@@ -491,7 +494,7 @@ int tdp_pages_fork(tdp_pages* h, const int32_t* parents, const int32_t* src_tabl
   const int rc = check_pages_device(h);
   if (rc != TDP_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
-  int* const rows = h->ints + 3 * h->chunks + 2;
+  int* const rows = h->ints + 3 * h->chunks + 3;
   const ForkArgs a{parents, src_tables, src_lens, add, n_src, add_all, n_dst, (int)W, (int)N, h->chunks, refs_in, refs_out, dst_tables, dst_lens,
                    copies, status, h->marks, h->ints, rows, rows + h->cfg.max_rows, rows + 2 * h->cfg.max_rows, h->ints + 3 * h->chunks};
   pages_survey_kernel<<<1 + h->chunks, 1024, 2 * (size_t)n_src * sizeof(int), s>>>(a);
@@ -515,11 +518,10 @@ int tdp_pages_compact(tdp_pages* h, const int32_t* src_tables, const int32_t* le
   const int rc = check_pages_device(h);
   if (rc != TDP_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
-  int* const per_page = h->ints + 3 * h->chunks + 2 + 3 * h->cfg.max_rows;
+  int* const per_page = h->ints + 3 * h->chunks + 3 + 3 * h->cfg.max_rows;
   const CompactArgs a{src_tables, lens, n_rows, h->cfg.max_pages_per_seq, (int)N, h->chunks, max_moves, refs_in, refs_out, dst_tables, moves, status,
                       h->marks, h->marks + (int64_t)h->chunks * kChunkWords, h->ints, h->ints + h->chunks, h->ints + 2 * h->chunks,
-                      per_page, per_page + N, per_page + 2 * N, h->ints + 3 * h->chunks};
-  compact_clear_kernel<<<(unsigned)((N + 255) / 256), 256, 0, s>>>(a);
+                      per_page, per_page + N, per_page + 2 * N, per_page + 3 * N, h->ints + 3 * h->chunks + 2};
   if (n_rows > 0) compact_count_kernel<<<n_rows, 256, 0, s>>>(a);
   compact_survey_kernel<<<h->chunks, 1024, 0, s>>>(a);
   compact_list_kernel<<<(h->chunks + 3) / 4, 256, 0, s>>>(a);

@@ -160,7 +160,9 @@ def test_compaction_of_random_tables(n_rows, width, count, longest, moves, in_pl
 
 
 def test_compaction_moves_nothing_where_a_row_is_refused():
+    """And the call behind that is what it would have been."""
     tables, lens, refs = [[7, 9, -1], [6, -1, -1]], [20, 3], [0] * 6 + [1, 1]
+    good = [[7, 6, -1], [6, -1, -1]], [20, 3], [0] * 6 + [2, 1]
     with Pages(8, 4, 3) as pages:
         for lens, tables in ((lens, tables), ([49, 3], [[7, 5, 4], [6, -1, -1]]), ([-1, 3], [[7, 5, 4], [6, -1, -1]])):
             t, r = i32(tables), torch.empty(8, dtype=torch.int32, device="cuda")
@@ -168,6 +170,10 @@ def test_compaction_moves_nothing_where_a_row_is_refused():
             tdp.tdp_pages_compact(pages.h, t, i32(lens), 2, 8, i32(refs), r, out, m, status)
             assert status.tolist() == [0, 1, 0, 2] and (m == -1).all() and r.tolist() == refs
             assert out.tolist() == P.compact(tables, lens, refs, 8, 3)[0]
+            t = i32(good[0])
+            tdp.tdp_pages_compact(pages.h, t, i32(good[1]), 2, 8, i32(good[2]), r, out, m, status)
+            assert (out.tolist(), r.tolist(), [tuple(x) for x in m.tolist()], tuple(status.tolist())) == P.compact(*good, 8, 3)
+            assert status.tolist() == [0, 0, 2, 2]
 
 
 @pytest.mark.parametrize("shape,kv_scales", [("tiny", None), ("tiny_gqa", (0.5, 0.25)), ("tiny_h128", None), ("tiny_mqa", (1.0, 1.0)), ("13b_quarter", None)])
