@@ -7,7 +7,8 @@ library (token embedding -> tdp_stage_prefill / tdp_stage_decode -> final norm +
 projection + greedy selection) and keeps every request's tokens.  The pipeline clock of the
 schedule still comes from the profiles handed to the scheduler; the work itself is done by the HIP
 kernels, on the stream the caller names, and so are the copies in front of them and behind them: ids and
-tables up, answers down.  Host logic only: no arithmetic of the method lives here.
+tables up, answers down.  BeamSearch, beside the worker, searches with several continuations of every prompt, whose
+tables the device itself forks.  Host logic only: no arithmetic of the method lives here.
 """
 from __future__ import annotations
 
@@ -201,3 +202,133 @@ class StageWorker:
             raise ValueError("requests and prompts disagree")
         return sched.tdp_simulate_exec(cfg, requests, decode_profile, prefill_profile, prefill=self.prefill,
                                        decode=self.decode, release=self.release, events_cap=events_cap)
+
+
+class BeamSearch:
+    """Beam search on a stage (or the stages of a pipeline held by one GPU) and a pair of pipeline ends: prompts are prefilled once, their
+    rows fork into `beams` rows, and every step decodes all beams with their shared prefixes read once, ranks the continuations of a
+    request's beams over the whole vocabulary, and forks the block tables accordingly.  Choices, tables and page copies stay on the
+    device: the host reads nothing between the steps but, every `stop_every` steps, whether all beams have ended.
+    It owns the pages of the stages while it runs.  Row b of a step is beam b % beams of request b // beams."""
+
+    def __init__(self, tdp, stage, ends: int, d_model: int, vocab_size: int, num_pages: int, max_pages_per_seq: int, max_batch: int,
+                 max_tokens: int, max_seqs: int, stream=None):
+        self.tdp, self.ends = tdp, ends
+        self.stages = [stage] if isinstance(stage, int) else list(stage)
+        self.d_model, self.vocab_size, self.num_pages, self.max_pps = d_model, vocab_size, num_pages, max_pages_per_seq
+        self.max_batch, self.max_tokens, self.max_seqs = max_batch, max_tokens, max_seqs
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self.torch_stream = (self.stream if isinstance(self.stream, torch.cuda.Stream)
+                             else torch.cuda.ExternalStream(getattr(self.stream, "cuda_stream", self.stream)))
+        rows = max(max_batch, max_seqs, 1)
+        self.pages = self.select = None
+        self.pages = tdp.tdp_pages_create(tdp.PagesConfig(num_pages, rows, max_pages_per_seq))
+        self.select = tdp.tdp_beams_create(tdp.BeamsConfig(rows, tdp.MAX_TOP))
+
+    def close(self) -> None:
+        """Gives the library's objects back."""
+        if self.pages:
+            self.tdp.tdp_pages_destroy(self.pages)
+        if self.select:
+            self.tdp.tdp_beams_destroy(self.select)
+        self.pages = self.select = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def generate(self, prompts: Sequence[Sequence[int]], beams: int, max_new: int, end_token: int = -1,
+                 stop_every: int = 8) -> List[List[Tuple[List[int], float]]]:
+        """For every prompt its beams, best first: (generated tokens, sum of their log-probabilities).  A beam that chose end_token keeps it as
+        its last token.  Beams that never had a continuation of their own (a vocabulary smaller than the beams) are left out."""
+        n = len(prompts)
+        if n < 1 or any(len(p) < 1 for p in prompts):
+            raise ValueError("every prompt needs a token")
+        if not 1 <= beams <= min(self.tdp.MAX_BEAMS, self.tdp.MAX_TOP, self.vocab_size) or max_new < 1 or stop_every < 1:
+            raise ValueError("beams must be 1 .. %d and within the vocabulary, max_new and stop_every at least 1" % self.tdp.MAX_TOP)
+        if not -1 <= end_token < self.vocab_size:
+            raise ValueError("end_token must be a token, or -1 for none")
+        total, rows = sum(map(len, prompts)), n * beams
+        if n > self.max_seqs or total > self.max_tokens or rows > self.max_batch:
+            raise ValueError("%d prompts, %d tokens, %d beams exceed the stage's limits" % (n, total, rows))
+        longest = max(map(len, prompts)) + max_new
+        if longest > PAGE * self.max_pps:
+            raise ValueError("%d tokens do not fit a block-table row" % longest)
+        # pages of the prompts, those that beams have of their own, and those that a step's new rows take before the old ones give theirs back
+        needed = sum(-(-len(p) // PAGE) for p in prompts) + rows * (-(-max_new // PAGE) + 1) + 2 * rows
+        if needed > self.num_pages:
+            raise OutOfPages("up to %d pages are needed, there are %d" % (needed, self.num_pages))
+        return self._generate([list(map(int, p)) for p in prompts], beams, max_new, end_token, stop_every)
+
+    @_on_own_stream
+    def _generate(self, prompts, beams, max_new, end_token, stop_every):
+        tdp, n, rows = self.tdp, len(prompts), len(prompts) * beams
+        total = sum(map(len, prompts))
+        i32 = StageWorker._i32
+
+        def ints(*shape):  # (zeros: whatever has not been written names a page that there is)
+            return torch.zeros(shape, dtype=torch.int32, device="cuda")
+        refs = torch.zeros(self.num_pages, dtype=torch.int32, device="cuda")
+        states = [(ints(max(rows, n), self.max_pps), ints(max(rows, n))) for _ in range(2)]  # tables and lengths, before and behind a fork
+        copies, status = ints(max(rows, n), 2), ints(max_new + 1, 4)
+        parents, tokens, ended = ints(max_new, rows), ints(max_new, rows), ints(max_new, rows)
+        scores = [torch.empty(rows, dtype=torch.float32, device="cuda") for _ in range(2)]
+        x = torch.empty((max(total, rows), self.d_model), dtype=torch.bfloat16, device="cuda")
+        y = torch.empty_like(x)
+        logits = torch.empty((rows, self.vocab_size), dtype=torch.float32, device="cuda")
+
+        # the prompts
+        lens = [len(p) for p in prompts]
+        cu = np.zeros(n + 1, dtype=np.int32)
+        cu[1:] = np.cumsum(lens)
+        cu_dev, (tables, table_lens) = i32(cu), states[0]
+        tdp.tdp_pages_fork(self.pages, None, None, None, 0, i32(lens), 0, n, refs, refs, tables, table_lens, copies, status[0], self.stream)
+        tdp.tdp_embed_tokens(self.ends, i32(sum(prompts, [])), total, x, self.stream)
+        for st in self.stages:
+            tdp.tdp_stage_prefill(st, x, cu_dev, tables, n, total, y, self.stream)
+            x, y = y, x
+        tdp.tdp_lm_head(self.ends, x, total, i32(cu[1:] - 1), n, logits, None, self.stream)
+        scores[0][:n] = 0
+        tdp.tdp_beams_select(self.select, logits, tdp.F32, n, 1, self.vocab_size, self.vocab_size, scores[0], None, end_token, beams, parents[0], tokens[0],
+                             scores[1], ended[0], self.stream)
+        # A row's length is that of the tokens that its pages have room for: with the one that is decoded next.
+        groups, step, n_src = i32(np.arange(n + 1) * beams), 0, n
+        while step + 1 < max_new:
+            (tables, table_lens), (new_tables, new_lens) = states[step % 2], states[(step + 1) % 2]
+            tdp.tdp_pages_fork(self.pages, parents[step], tables, table_lens, n_src, None, 1, rows, refs, refs, new_tables, new_lens, copies,
+                               status[step + 1], self.stream)
+            for st in self.stages:
+                tdp.tdp_stage_kv_copy_pages(st, copies, rows, self.stream)
+            if (step + 1) % stop_every == 0 and bool((status[:step + 2, :2] != 0).any() | (ended[step] != 0).all()):
+                break
+            ctx = new_lens - 1
+            tdp.tdp_embed_tokens(self.ends, tokens[step], rows, x, self.stream)
+            for st in self.stages:
+                tdp.tdp_stage_decode_shared(st, x, ctx, new_tables, rows, groups, n, y, self.stream)
+                x, y = y, x
+            tdp.tdp_lm_head(self.ends, x, rows, None, rows, logits, None, self.stream)
+            step, n_src = step + 1, rows
+            tdp.tdp_beams_select(self.select, logits, tdp.F32, n, beams, self.vocab_size, self.vocab_size, scores[step % 2],
+                                 ended[step - 1] if end_token >= 0 else None, end_token, beams, parents[step], tokens[step], scores[(step + 1) % 2],
+                                 ended[step], self.stream)
+        if bool((status[:step + 1, :2] != 0).any()):
+            raise OutOfPages("a fork of the block tables found no page")
+        parents, tokens, final = parents[:step + 1].cpu().tolist(), tokens[:step + 1].cpu().tolist(), scores[(step + 1) % 2].cpu().tolist()
+        answers = []
+        for g in range(n):
+            answers.append([])
+            for row in range(g * beams, (g + 1) * beams):
+                found, at = [], row
+                for s in range(step, -1, -1):
+                    if at < 0 or tokens[s][at] < 0:
+                        break
+                    found.append(tokens[s][at])
+                    at = parents[s][at]
+                else:
+                    found.reverse()
+                    if end_token in found:
+                        found = found[:found.index(end_token) + 1]
+                    answers[g].append((found, final[row]))
+        return answers
