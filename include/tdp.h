@@ -464,7 +464,7 @@ TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_r
  * infinity, finished_out 0.  The candidates are compared in 64 bits: a row's sum of exponentials is formed in fp32 per thread (64 terms at
  * most) and joined in 64.
  *   logits   dev, TDP_F32 or TDP_BF16, [n_groups * beams][n], rows ld >= n elements apart, at any alignment of their type
- *   scores   dev fp32 [n_groups * beams]
+ *   scores   dev fp32 [n_groups * beams], not overlapping score
  *   finished dev int32 [n_groups * beams], not 0: finished; or null.  end_token: in [0, n), or, with finished null, -1: none
  * beams 1 .. TDP_MAX_BEAMS, n_out 1 .. TDP_MAX_TOP and at most beams * n, n up to 2^27, n_groups * beams <= max_rows (0: nothing to do).
  * A tdp_beams owns scratch.  It lives on the device that is current when it is created, calls on it need that device current, and it must

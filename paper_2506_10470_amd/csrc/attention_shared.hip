@@ -53,6 +53,7 @@ struct PlanArgs {
 constexpr int kPlanThreads = 256, kPlanRows = 32;  // rows that a workgroup compares, as long as there are not too many workgroups
 constexpr int kPlanHeld = 1024;                    // rows, and groups, that the last workgroup holds in LDS
 constexpr int kClasses = 17;                       // of row spans by their length
+typedef i32x4 __attribute__((aligned(4))) i32x4_of_int;
 __device__ __forceinline__ int row_tokens(const SharedBatch& b, int r) { return min(max(b.lens[r], 0) + b.add, b.max_pages_per_seq * 16); }
 
 // A thread's value plus those of all threads of the workgroup in front of it, and the sum of all.
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
   constexpr int T = kPlanThreads;
   __shared__ int32_t s_starts[kPlanHeld + 1], s_tokens[kPlanHeld], s_group[4 * kPlanHeld], s_pages[T], s_first[T];
   __shared__ int is_last, longest_limit, part[T / 64], class_at[kClasses];
-  __shared__ unsigned work;
+  __shared__ unsigned long long work;
   const SharedBatch& b = a.b;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, P = b.max_pages_per_seq, n_groups = b.n_groups;
   const bool few = n_groups <= kPlanHeld, held = b.batch <= kPlanHeld;
@@ -127,7 +128,9 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
           limit = (own_tokens - 1) >> 4;
           int tokens = 0;
           for (first = begin_of(g); first < r && (tokens = tokens_of(first)) <= 0;) ++first;
-          if (first < r) {
+          if (first < r && P < 4) {
+            limit = 0;  // (tables of three entries have nothing worth sharing, nor four entries to look at at once)
+          } else if (first < r) {
             limit = min(limit, (tokens - 1) >> 4);
             atomicMax(&longest_limit, limit);
           }
@@ -136,29 +139,27 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
         s_first[tid] = first;
       }
       __syncthreads();
-      // the first difference from that row: a wave compares eight rows' 256 entries at a time, low pages first
-      constexpr int ROWS = 8, PART = 4;
-      const int chunks = (longest_limit + 64 * PART - 1) / (64 * PART), eights = (rows + ROWS - 1) / ROWS;
+      // the first difference from that row: a wave compares eight rows' 256 entries at a time, four side by side to a lane, low pages first
+      constexpr int ROWS = 8, SIDE = 4;
+      const int chunks = P >= SIDE ? (longest_limit + 64 * SIDE - 1) / (64 * SIDE) : 0, eights = (rows + ROWS - 1) / ROWS;
       for (int i = wave; i < eights * chunks; i += T / 64) {
-        const int c = i / eights, at = c * 64 * PART + lane, row0 = (i - c * eights) * ROWS;
-        int limit[ROWS], want[ROWS][PART], got[ROWS][PART];
+        const int c = i / eights, row0 = (i - c * eights) * ROWS;
+        int limit[ROWS], at[ROWS];
+        i32x4 want[ROWS], got[ROWS];
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
           const int row = min(row0 + j, rows - 1), of = s_first[row];
           limit[j] = of == t0 + row ? 0 : *(volatile int*)&s_pages[row];
-#pragma unroll
-          for (int u = 0; u < PART; ++u) {  // (in bounds, and not used where a row has nothing to compare)
-            const int e = min(at + u * 64, max(limit[j], 1) - 1);
-            want[j][u] = b.block_tables[(int64_t)of * P + e];
-            got[j][u] = b.block_tables[(int64_t)(t0 + row) * P + e];
-          }
+          at[j] = min((c * 64 + lane) * SIDE, max(limit[j], SIDE) - SIDE);  // (in the row, and not used where there is nothing to compare)
+          want[j] = *reinterpret_cast<const i32x4_of_int*>(b.block_tables + (int64_t)of * P + at[j]);
+          got[j] = *reinterpret_cast<const i32x4_of_int*>(b.block_tables + (int64_t)(t0 + row) * P + at[j]);
         }
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
           int differs = 0x7fffffff;
 #pragma unroll
-          for (int u = PART - 1; u >= 0; --u)
-            if (got[j][u] != want[j][u]) differs = min(at + u * 64, limit[j] - 1);
+          for (int u = SIDE - 1; u >= 0; --u)
+            if (got[j][u] != want[j][u]) differs = at[j] + u;
           if (differs < limit[j]) atomicMin(&s_pages[min(row0 + j, rows - 1)], differs);
         }
       }
@@ -210,11 +211,12 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
     // has no more slots for partials than spans of that length.
     if (last[g] <= first[g] || (pages < kMinSpanPages && longest[g] - pages * 16 > kDecodeSpanMin)) pages = 0;
     common[g] = pages;
-    if (pages) atomicAdd(&work, (unsigned)tiles_of(g) * pages);  // (below 2^32: no more rows than pages of 32 bits name)
+    if (pages) atomicAdd(&work, (unsigned long long)tiles_of(g) * (unsigned long long)pages);
   }
   __syncthreads();
   // prefixes in spans as long as the number wanted allows, all of a group equally long; their items, a thread each
-  const int span = max((unsigned)kMinSpanPages, (work + a.wanted - 1) / a.wanted);
+  const unsigned long long all_pages = work + a.wanted - 1;  // (a division of 32 bits where that is enough: a fifth of the time)
+  const int span = max(kMinSpanPages, (int)(all_pages >> 32 ? all_pages / (unsigned)a.wanted : (unsigned)all_pages / (unsigned)a.wanted));
   auto spans_of = [&](int pages) { return pages > 0 ? max(1, min((pages + span - 1) / span, pages / kMinSpanPages)) : 0; };
   int base = 0;
   for (int g0 = 0; g0 < n_groups; g0 += T) {
@@ -295,7 +297,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
 // SPLIT: the four waves of a workgroup share the span out; otherwise each has one of its own, with no LDS and no barrier: short spans by
 // the thousand are mostly their own beginning and end.
 template <int DH, bool KV8, bool PREFIX, bool SPLIT>
-__global__ __launch_bounds__(256, KV8 && DH == 128 ? 2 : 3) void attn_columns_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
+__global__ __launch_bounds__(256, (KV8 || SPLIT) && DH == 128 ? 2 : 3) void attn_columns_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
                                                               const int4* __restrict__ items, const int32_t* __restrict__ count,
                                                               const int32_t* __restrict__ block_tables, int max_pages_per_seq,
                                                               float* __restrict__ part_o, float* __restrict__ part_ml,
@@ -701,21 +703,19 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
   constexpr int NCH = BLK * CR / 256;                      // 8-element chunks of K, and of V, per thread
   constexpr int TPI = 512 / DH, NJ = 16 / TPI;             // keys of an instruction, instructions of a page
   constexpr int WPH = 4 / NH, NV = DH / WPH / 16;          // waves of a half of V, instructions of one
-  constexpr int KP = KV8 ? NCH : NPG / 4, VP = KV8 ? NCH : 1;
+  constexpr int KP = KV8 ? NPG : NPG / 4;
   const int v_row = lane >> 2, v_chunk = (lane & 3) ^ ((v_row >> 2) & 3);
-  int k_page[KP], v_page[VP];  // those that this thread asks for something of
+  // the pages that this thread asks for something of: of keys those of its wave, of values its own (8 bits: all of the block, for both)
+  int k_page[KP], v_page = 0;
   auto look_up = [&](int b) {
     auto id = [&](int i) { return table[min(b * NPG + i, n_pages - 1)]; };
     if constexpr (KV8) {
 #pragma unroll
-      for (int j = 0; j < NCH; ++j) {
-        k_page[j] = id((tid + 256 * j) / (16 * CR));
-        v_page[j] = id(256 * j / (DH * 4) * 2 + ((tid & 3) >> 1));
-      }
+      for (int p = 0; p < KP; ++p) k_page[p] = __builtin_amdgcn_readfirstlane(id(p));
     } else {
 #pragma unroll
       for (int p = 0; p < KP; ++p) k_page[p] = id(w * KP + p);
-      v_page[0] = id(w / WPH * 2 + (v_chunk >> 1));
+      v_page = id(w / WPH * 2 + (v_chunk >> 1));
     }
   };
   uint2 kraw[KV8 ? NCH : 1], vraw[KV8 ? NCH : 1];
@@ -736,8 +736,11 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
         // pieces of the row, the pages of the block
         const int kq = ci % 8, kt16 = (ci / 8) % 16, kpiece = (ci / 128) % (CR / 8);
         const int vr = (ci >> 2) % DH, vc = ci & 3;
-        kraw[j] = *reinterpret_cast<const uint2*>((const uint8_t*)kv.k_pool + ((int64_t)k_page[j] * Hkv + kvh) * HEAD + (kpiece * 16 + kt16) * 64 + kq * 8);
-        vraw[j] = *reinterpret_cast<const uint2*>((const uint8_t*)kv.v_pool + (((int64_t)v_page[j] * Hkv + kvh) * DH + vr) * 16 + (vc & 1) * 8);
+        constexpr int PER = 256 / (16 * CR);  // pages of 256 chunks of keys: 1 or 2
+        const int kp = PER == 1 ? k_page[j] : w < 2 ? k_page[(PER * j) % KP] : k_page[(PER * j + 1) % KP];
+        const int v0 = k_page[256 * j / (DH * 4) * 2], v1 = k_page[256 * j / (DH * 4) * 2 + 1], vp = vc < 2 ? v0 : v1;
+        kraw[j] = *reinterpret_cast<const uint2*>((const uint8_t*)kv.k_pool + ((int64_t)kp * Hkv + kvh) * HEAD + ((kpiece * 16 + kt16) * 64 + kq * 8));
+        vraw[j] = *reinterpret_cast<const uint2*>((const uint8_t*)kv.v_pool + ((int64_t)vp * Hkv + kvh) * HEAD + (vr * 16 + (vc & 1) * 8));
       }
     } else {
 #pragma unroll
@@ -751,7 +754,7 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
         }
       }
       const int half = w / WPH, part = w % WPH;
-      const bf16* vp = (const bf16*)kv.v_pool + ((int64_t)v_page[0] * Hkv + kvh) * HEAD + (part * (DH / WPH) + v_row) * 16 + (v_chunk & 1) * 8;
+      const bf16* vp = (const bf16*)kv.v_pool + ((int64_t)v_page * Hkv + kvh) * HEAD + (part * (DH / WPH) + v_row) * 16 + (v_chunk & 1) * 8;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
         request(v_lds + ((buf * NH + half) * HALF + (part * (DH / WPH) + j * 16) * 32) * 2, vp + j * 256);
@@ -819,14 +822,17 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) sc = mfma32(kf[kk], qf[kk], sc);
       __builtin_amdgcn_sched_barrier(0);
-      bf16x8 vf[DT][2];  // on their way during the softmax
+      // on their way during the softmax (8-bit pools, whose codes wait in registers: a quarter of them)
+      constexpr int VD = KV8 && NWC == 4 && DT > 2 ? 1 : DT;
+      bf16x8 vf[VD][2];
+      auto fragment = [&](int d, int st) {
+        const int r = d * 32 + l32;
+        return ld_bf16x8(vh + r * 32 + (((st * 2 + kg) ^ ((r >> 2) & 3)) << 3));
+      };
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < VD; ++d)
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          const int r = d * 32 + l32;
-          vf[d][st] = ld_bf16x8(vh + r * 32 + (((st * 2 + kg) ^ ((r >> 2) & 3)) << 3));
-        }
+        for (int st = 0; st < 2; ++st) vf[d][st] = fragment(d, st);
       __builtin_amdgcn_sched_barrier(0);
       // element i of this lane is token kb + (i/8)*16 + kg*8 + i%8 of its column
       if (kb + 32 > n_tokens) {  // (an odd number of pages)
@@ -859,7 +865,7 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int st = 0; st < 2; ++st) o[d] = mfma32(vf[d][st], pb[st], o[d]);
+        for (int st = 0; st < 2; ++st) o[d] = mfma32(d < VD ? vf[d < VD ? d : 0][st] : fragment(d, st), pb[st], o[d]);
     }
     if (more) settle(b + 1, buf ^ 1);
   }
