@@ -18,23 +18,30 @@ constexpr int kMinSpanPages = kDecodeSpanMin / 16;
 constexpr int kResident = 3 * 256;  // workgroups of the sixteen-column kernel that the chip holds at once
 
 // How a batch is attended to: a pure function of sizes that the host knows.
+//
+// columns: of a tile of the prefix kernel, by the average group's.  Four groups with a prefix of 2400 to 4000 tokens, 8 K/V heads of 128
+// channels, 8 query heads to each, the whole call, tiles of 16 / 64 / 128 columns: groups of 24 columns 39 / 48 / 49 us, 32 46 / 53 / 54, 48
+// 48 / 53 / 55, 64 56 / 55 / 56, 96 59 / 63 / 58, 128 63 / 64 / 59, 512 138 / 114 / 106; 8-bit pools 32 47 / 45 / 45, 48 51 / 47 / 49, 64 60 / 49 /
+// 51; 64 groups of 32 152 / 172 / 182, of 48 203 / 183 / 197.
+// wanted: spans of the prefixes per K/V head (spans of a group times its tiles), as many as make the workgroups that the chip holds at once,
+// twice that for 64 columns.  16 columns, 512 / 768 / 1536 / 3072 workgroups: 8 groups of 8000 tokens, 32 heads 153 / 151 / 155 / 166 us, 32 of 1500
+// 135 / 135 / 141 / 148; 128 columns, 512 rows behind one prompt of 2100, 256 / 512 / 768 / 1536: 157 / 143 / 156 / 170.
 struct Form {
-  int columns;      // of a tile of the prefix kernel: 16, 32, 64 or 128, by the average group
-  bool split;       // 16 columns: the waves of a workgroup share a span's tokens out, instead of taking a span each
-  int wanted;       // spans of the prefixes per K/V head (spans of a group times its tiles)
+  int columns, wanted;
 };
-// Whether the waves of a workgroup share a row's span out as well.
-bool rows_split(int batch, int n_kv_heads) { return (int64_t)batch * n_kv_heads < 1024; }
 Form form_of(int batch, int n_groups, int n_q_heads, int n_kv_heads) {
   const int G = n_q_heads / n_kv_heads;
   const int64_t average = n_groups > 0 ? ((int64_t)batch * G + n_groups - 1) / n_groups : 0;
   Form f;
-  f.columns = average <= 16 ? 16 : average <= 32 ? 32 : average <= 64 ? 64 : 128;
-  f.split = (int64_t)n_groups * n_kv_heads < 1024;
-  const int units = f.columns == 16 ? (f.split ? 2 * kResident : 8 * kResident) : f.columns == 32 ? 1024 : f.columns == 64 ? 1024 : 512;
+  f.columns = average <= 32 ? 16 : average <= 64 ? 64 : 128;
+  const int units = f.columns == 16 ? kResident : f.columns == 64 ? 1024 : 512;
   f.wanted = (units + n_kv_heads - 1) / n_kv_heads;
   return f;
 }
+// Whether the waves of a workgroup share a row's span out, or have one each.  Own tokens of up to 100 / 400 / 1000 (whole calls, 8 K/V heads,
+// shared out against one each): 32 rows 31 / 34 us and 28 / 42, 64 rows 35 / 37 and 34 / 44, 128 rows 42 / 39 and 46 / 48, 256 rows 56 / 49, 70 / 69
+// and 121 / 132, 512 rows 90 / 74, 119 / 116 and 217 / 225; 8-bit pools, up to 200, 96 rows 41 / 40, 256 rows 61 / 49.
+bool rows_split(int batch, int n_kv_heads) { return (int64_t)batch * n_kv_heads < 1024; }
 int items_of(const SharedBatch& b, const Form& f) {
   return (int)((int64_t)b.batch * (b.n_q_heads / b.n_kv_heads) / f.columns) + b.n_groups + f.wanted;
 }
@@ -50,7 +57,7 @@ struct PlanArgs {
   int32_t* counts;
   int4 *prefix_items, *row_items;
 };
-constexpr int kPlanThreads = 256, kPlanRows = 32;  // rows that a workgroup compares, as long as there are not too many workgroups
+constexpr int kPlanThreads = 256, kPlanRows = 16;  // rows that a workgroup compares, as long as there are not too many workgroups
 constexpr int kPlanHeld = 1024;                    // rows, and groups, that the last workgroup holds in LDS
 constexpr int kClasses = 17;                       // of row spans by their length
 typedef i32x4 __attribute__((aligned(4))) i32x4_of_int;
@@ -295,7 +302,8 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
 // heads of one row, the span one of what it has behind its prefix; the prefix's partials, and those of the row's other spans if it has some
 // (whoever is done last), are combined with them.
 // SPLIT: the four waves of a workgroup share the span out; otherwise each has one of its own, with no LDS and no barrier: short spans by
-// the thousand are mostly their own beginning and end.
+// the thousand are mostly their own beginning and end.  Prefixes are always shared out (a span each: up to 20 % slower, but for some 256 to 512
+// short 8-bit prefixes, where it was 3 % faster).
 template <int DH, bool KV8, bool PREFIX, bool SPLIT>
 __global__ __launch_bounds__(256, (KV8 || SPLIT) && DH == 128 ? 2 : 3) void attn_columns_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
                                                               const int4* __restrict__ items, const int32_t* __restrict__ count,
@@ -635,19 +643,19 @@ __global__ __launch_bounds__(256, (KV8 || SPLIT) && DH == 128 ? 2 : 3) void attn
 
 // ---- many columns ------------------------------------------------------------------------------------------------------------
 
-// One workgroup of four waves per (item, K/V head).  NWC waves have 32 columns each, and 4 / NWC waves share the tokens of a block out for
-// the same columns.  A block of 64 tokens (128 for one wave of columns) of K and V^T is staged in LDS, double buffered and swizzled,
+// One workgroup of four waves per (item, K/V head).  NWC waves, two or four, have 32 columns each, and 4 / NWC waves share the tokens of a block
+// out for the same columns.  A block of 64 tokens of K and V^T is staged in LDS, double buffered and swizzled,
 // and feeds the 32x32x16 MFMAs of all columns; scores are formed transposed, with their rows permuted so that a lane's elements are the
 // consecutive tokens that it supplies to O^T += V^T P^T, as in the prefill kernel, whose masks are not needed here: a prefix is whole pages.
 // Bound: reading the pages up to about a hundred columns, MFMA beyond.
 template <int DH, int NWC, bool KV8>
-__global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
+__global__ __launch_bounds__(256, 2) void attn_prefix_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
                                                                             const int4* __restrict__ items, const int32_t* __restrict__ count,
                                                                             const int32_t* __restrict__ block_tables, int max_pages_per_seq,
                                                                             float* __restrict__ part_o, float* __restrict__ part_ml,
                                                                             int max_spans, float scale_log2) {
   constexpr int NWT = 4 / NWC;               // waves that share the tokens out
-  constexpr int NH = NWC == 1 ? 4 : 2;       // 32-token halves of a block
+  constexpr int NH = 2;                      // 32-token halves of a block
   constexpr int BLK = 32 * NH, NPG = BLK / 16;
   constexpr int KS = DH / 16, DT = DH / 32;  // k-steps of the scores, 32-channel tiles of the output
   constexpr int CR = DH / 8;                 // 16-byte chunks of a key in LDS
@@ -923,12 +931,13 @@ __global__ __launch_bounds__(256, NWC == 1 ? 1 : 2) void attn_prefix_kernel(cons
 }  // namespace
 
 int attn_prefix_items_most(int max_batch, int n_q_heads, int n_kv_heads) {
-  return max_batch * (n_q_heads / n_kv_heads) / 16 + max_batch + (8 * kResident + n_kv_heads - 1) / n_kv_heads;
+  return max_batch * (n_q_heads / n_kv_heads) / 16 + max_batch + (1024 + n_kv_heads - 1) / n_kv_heads;
 }
 
-// Spans of what rows have behind their prefix: as in decode attention where four waves share one, shorter where each is a wave's.
+// Spans of what rows have behind their prefix: as in decode attention where four waves share one, shorter where each is a wave's (512 / 1024 /
+// 2048 tokens, 8 K/V heads: 256 rows of up to 400 tokens 78 / 69 / 69 us, 512 of up to 1000 259 / 225 / 225; 16 rows of 64 heads, up to 1000, 54 / 64 / 65).
 int attn_shared_span(int batch, int n_kv_heads) {
-  return rows_split(batch, n_kv_heads) ? attn_decode_span(batch, n_kv_heads) : (int64_t)batch * n_kv_heads >= 4096 ? 1024 : 512;
+  return rows_split(batch, n_kv_heads) ? attn_decode_span(batch, n_kv_heads) : 1024;
 }
 
 hipError_t launch_attn_shared_plan(const SharedBatch& b, const SharedScratch& sc, hipStream_t s) {
@@ -956,12 +965,6 @@ hipError_t launch_attn_shared(const SharedBatch& b, const SharedScratch& sc, con
   attn_columns_kernel<DH, KV8, PREFIX, SPLIT><<<grid, 256, 0, s>>>((const bf16*)q, ld, b.n_q_heads, kv, items, count, b.block_tables,    \
                                                                    b.max_pages_per_seq, part_o, part_ml, spans_done, max_spans, b.span_len, \
                                                                    (bf16*)out, out_layout, scale_log2, out_scale)
-#define TDP_COLUMNS(DH, KV8, PREFIX, split, units, items, count)                            \
-  do {                                                                                      \
-    const unsigned grid = grid_of(units, split);                                            \
-    if (split) TDP_COLUMNS_(DH, KV8, PREFIX, true, grid, items, count);                     \
-    else TDP_COLUMNS_(DH, KV8, PREFIX, false, grid, items, count);                          \
-  } while (0)
 #define TDP_PREFIX_(DH, NWC, KV8)                                                                                                   \
   attn_prefix_kernel<DH, NWC, KV8><<<(unsigned)prefix_units, 256, 0, s>>>((const bf16*)q, ld, b.n_q_heads, kv, sc.prefix_items, sc.counts, \
                                                                           b.block_tables, b.max_pages_per_seq, part_o, part_ml, max_spans, \
@@ -969,12 +972,14 @@ hipError_t launch_attn_shared(const SharedBatch& b, const SharedScratch& sc, con
 #define TDP_SHARED(DH, KV8)                                                                                   \
   do {                                                                                                        \
     if (b.n_groups > 0) {                                                                                     \
-      if (f.columns == 16) TDP_COLUMNS(DH, KV8, true, f.split, prefix_units, sc.prefix_items, sc.counts);     \
-      else if (f.columns == 32) TDP_PREFIX_(DH, 1, KV8);                                                      \
+      if (f.columns == 16)                                                                                    \
+        TDP_COLUMNS_(DH, KV8, true, true, grid_of(prefix_units, true), sc.prefix_items, sc.counts);           \
       else if (f.columns == 64) TDP_PREFIX_(DH, 2, KV8);                                                      \
       else TDP_PREFIX_(DH, 4, KV8);                                                                           \
     }                                                                                                         \
-    TDP_COLUMNS(DH, KV8, false, rows_alone, row_units, sc.row_items, sc.counts + 1);                        \
+    const unsigned rows_grid = grid_of(row_units, rows_alone);                                                \
+    if (rows_alone) TDP_COLUMNS_(DH, KV8, false, true, rows_grid, sc.row_items, sc.counts + 1);               \
+    else TDP_COLUMNS_(DH, KV8, false, false, rows_grid, sc.row_items, sc.counts + 1);                         \
   } while (0)
   if (kv.head_dim == 128) {
     if (kv.fp8) TDP_SHARED(128, true); else TDP_SHARED(128, false);
@@ -983,7 +988,6 @@ hipError_t launch_attn_shared(const SharedBatch& b, const SharedScratch& sc, con
   }
 #undef TDP_SHARED
 #undef TDP_PREFIX_
-#undef TDP_COLUMNS
 #undef TDP_COLUMNS_
   return hipGetLastError();
 }

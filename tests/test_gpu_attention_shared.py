@@ -117,7 +117,7 @@ def test_groups_of_many_kinds(heads, kv_scales):
 @pytest.mark.parametrize("heads", ["4/4x64", "8/2x64", "3/3x128", "16/2x128"])
 @pytest.mark.parametrize("rows", [2, 5, 9, 33])
 def test_prefixes_of_every_length_around_a_block(heads, rows, kv_scales):
-    """Tiles of 32, 64 and 128 columns, prefixes that end in every page of a block."""
+    """Tiles of 16, 64 and 128 columns, prefixes that end in every page of a block."""
     for pages in (1, 2, 3, 4, 5, 7, 8, 9, 15, 16, 17, 31, 32, 33, 49):
         with Cache(HEADS[heads], [(pages * PAGE + pages % 3, [1 + 3 * i % 20 for i in range(rows)])], pages, kv_scales) as c:
             c.check(c.attend())
@@ -187,6 +187,56 @@ def test_identical_tables_share_all_but_the_last_page():
                 torch.cuda.synchronize()
                 for b in range(6):
                     c.check(out[b:b + 1])
+
+
+def repeated(c, times, starts_of, span=0):
+    """The rows of a cache several times over, with the same queries: {number of groups: output}, for each list of starts."""
+    batch, (hq, hkv, dh) = c.batch * times, c.heads
+    with Stage(tdp, c.stage.shape, c.count, batch, 0, 0, c.width, load_weights=False) as st:
+        for a, b in zip(st.raw_pools(0), c.stage.raw_pools(0)):
+            a.copy_(b)
+        if span:
+            tdp.tdp_stage_set_decode_span(st.h, span)
+        q, lens, tables = c.q.cuda().repeat(times, 1, 1), i32(c.lens).repeat(times), i32(c.tables).repeat(times, 1)
+        for starts in starts_of:
+            out = torch.full_like(q, float("nan"))
+            tdp.tdp_stage_attend(st.h, 0, q, lens, tables, batch, i32(starts) if starts else None, max(0, len(starts) - 1), out)
+            torch.cuda.synchronize()
+            yield out.view(times, c.batch, hq, dh)
+
+
+@pytest.mark.parametrize("span", [0, 256])
+@pytest.mark.parametrize("heads,times", [("4/4x64", 420), ("6/3x128", 260), ("16/1x64", 1100)])
+def test_more_rows_and_groups_than_one_workgroup_holds(heads, times, span):
+    """Over 1024 rows, and over 1024 groups, some of whose rows have several spans."""
+    groups = [(272, [1, 30]), (0, [3]), (600, [1300, 16])]
+    with Cache(HEADS[heads], groups, 13) as c:
+        n = c.batch * times
+        every = [5 * t + s for t in range(times) for s in (0, 2, 3)] + [n]
+        assert n > 1024 and (len(every) > 1025) == (times > 341)
+        for out in repeated(c, times, (every, [], list(range(n + 1)), [0, 2, 2, 3, 5]), span):
+            c.check(out[0])
+            c.check(out[-1])
+            assert (out[1:-1] == out[1:2]).all()
+            c.check(out[1])
+
+
+def test_one_group_of_more_rows_than_the_comparing_workgroups_hold():
+    with Cache((2, 1, 64), [(64, [1, 9, 17, 33, 2])], 14) as c:
+        for out in repeated(c, 3400, ([0, 5 * 3400], [0, 3, 5 * 3400 - 2, 5 * 3400])):
+            c.check(out[0])
+            c.check(out[-1])
+            assert (out[1:-1] == out[1:2]).all()
+            c.check(out[1])
+
+
+def test_a_span_of_more_pages_than_a_wave_holds_at_once():
+    """Thirteen groups behind 262 to 300 pages, 64 heads: a span each."""
+    for pages in (262, 300):
+        with Cache((64, 64, 64), [(pages * PAGE, [5, 20])], 15) as c:
+            for out in repeated(c, 13, ([2 * g for g in range(14)],)):
+                c.check(out[0])
+                assert (out == out[:1]).all()
 
 
 def test_infinite_and_missing_numbers_stay_where_they_are():
@@ -312,3 +362,55 @@ def test_a_decode_step_with_groups_is_the_decode_step(shape, kv_scales, micro):
     (want, pools), (got, pools2) = results
     assert row_rel_err(got, want) <= TOL
     assert all(torch.equal(a, b) for a, b in zip(pools, pools2))
+
+
+def test_a_captured_decode_step_with_groups_follows_its_tables():
+    """Replays with other lengths and tables, eager steps between them, each against the step without groups."""
+    sh = W.SHAPES["tiny_gqa"]
+    rng, count, width, rows = np.random.default_rng(4), 90, 24, 6
+    hidden = W.hidden_states(sh, rows, 78, device="cuda")
+    starts = i32([0, 4, 6])
+
+    def batch(turn):
+        ids = rng.permutation(count).tolist()
+        tables, lens = np.zeros((rows, width), np.int32), []
+        for b, (group, own) in enumerate(zip((0, 0, 0, 0, 1, 1), (4, 20, 1, 9, 30, 2))):
+            if b in (0, 4):
+                common = [ids.pop() for _ in range((2 + turn) * (group + 1))]
+            n = len(common) * PAGE + own
+            row = common + [ids.pop() for _ in range(n // PAGE + 1 - len(common))]
+            tables[b, :len(row)] = row
+            lens.append(n)
+        return i32(lens), i32(tables)
+
+    with Stage(tdp, sh, count, rows, 0, 0, width) as st, Stage(tdp, sh, count, rows, 0, 0, width) as other:
+        g = torch.Generator(device="cuda").manual_seed(6)
+        for l in range(sh.n_layers):
+            for a, b in zip(st.raw_pools(l), other.raw_pools(l)):
+                a.copy_(torch.randn(a.shape, generator=g, device="cuda").bfloat16())
+                b.copy_(a)
+        lens, tables = batch(0)
+        out, want = torch.empty_like(hidden), torch.empty_like(hidden)
+
+        def step(stream=None):
+            tdp.tdp_stage_decode_shared(st.h, hidden, lens, tables, rows, starts, 2, out, stream)
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(torch.cuda.current_stream())
+        for turn in range(4):
+            for old, new in zip((lens, tables), batch(turn)):
+                old.copy_(new)
+            for l in range(sh.n_layers):
+                for a, b in zip(st.raw_pools(l), other.raw_pools(l)):
+                    b.copy_(a)
+            out.fill_(float("nan"))
+            graph.replay()
+            tdp.tdp_stage_decode(other.h, hidden, lens, tables, rows, want)
+            torch.cuda.synchronize()
+            assert row_rel_err(out.double().cpu().numpy(), want.double().cpu().numpy()) <= TOL
+            replayed = out.clone()
+            step()
+            torch.cuda.synchronize()
+            assert torch.equal(replayed, out)

@@ -17,5 +17,5 @@ def test_nothing_is_spilled(code_objects):  # noqa: F811
                 if name in field["name"]:
                     found.setdefault(name, []).append((int(field["vgpr_spill_count"]), int(field["private_segment_fixed_size"])))
     assert sorted(found) == sorted(NAMES)
-    assert len(found["attn_columns_kernel"]) == 16 and len(found["attn_prefix_kernel"]) == 12
+    assert len(found["attn_columns_kernel"]) == 12 and len(found["attn_prefix_kernel"]) == 8
     assert all(use == (0, 0) for uses in found.values() for use in uses), found
