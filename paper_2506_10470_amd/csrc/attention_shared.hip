@@ -15,7 +15,7 @@ namespace tdp {
 namespace {
 
 constexpr int kMinSpanPages = kDecodeSpanMin / 16;
-constexpr int kResident = 3 * 256;  // workgroups of the sixteen-column kernel that the chip holds at once
+constexpr int kResident = 3 * 256;  // workgroups of the sixteen-column kernel that the chip holds at once (two to three per CU)
 
 // How a batch is attended to: a pure function of sizes that the host knows.
 //
@@ -98,7 +98,9 @@ __device__ __forceinline__ int last_not_above(const int32_t* at, int n, int v) {
 // row items: (row, pages of the prefix, tokens behind it, span | spans of the prefix << 16)).  Results of other workgroups, which run on
 // other XCDs, are stored and read past the caches, and counted when they have arrived.
 // Rows of length zero attend to nothing: what their tables hold is not looked at.
-// Bound: a chain of look-ups and barriers (a workgroup alone: 5 us), and the tables, which one CU reads at some 30 GB/s.
+// Bound: a chain of look-ups and barriers (a workgroup alone: 5 us), and the tables, which one CU reads at some 30 GB/s.  4 rows 7 us; 162 rows in
+// 24 groups, 250 pages 13 us (loads 3, comparison 3, groups' sums 3, prefix items 2, row items 2); 512 rows in one group 15 us.  A workgroup per
+// 8 / 16 / 32 / 64 rows, the whole call: 512 rows behind one prompt 140 / 140 / 142 / 146 us, 24 groups of 8 157 / 157 / 159 / 162, 256 rows 55 / 55 / 56 / 62.
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArgs a) {
   constexpr int T = kPlanThreads;
   __shared__ int32_t s_starts[kPlanHeld + 1], s_tokens[kPlanHeld], s_group[4 * kPlanHeld], s_pages[T], s_first[T];
@@ -303,9 +305,13 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
 // (whoever is done last), are combined with them.
 // SPLIT: the four waves of a workgroup share the span out; otherwise each has one of its own, with no LDS and no barrier: short spans by
 // the thousand are mostly their own beginning and end.  Prefixes are always shared out (a span each: up to 20 % slower, but for some 256 to 512
-// short 8-bit prefixes, where it was 3 % faster).
+// short 8-bit prefixes, where it was 7 to 9 % faster).
+//
+// Bound: reading.  24 prefixes of 2400 to 4000 tokens, 32 heads of 128 8-bit channels 105 us (588 MB, 5.6 TB/s); what 512 rows of 8 heads have behind
+// their prefix, 15 to 312 tokens, 69 us (332 MB, and 34 MB of partials, 5.3 TB/s; with 168 registers for three waves to a SIMD instead of what two
+// allow 71 us; begun from the prefix's partials instead of ended with them 71 us; ordinary instead of non-temporal loads 85, and 119 for the 105).
 template <int DH, bool KV8, bool PREFIX, bool SPLIT>
-__global__ __launch_bounds__(256, (KV8 || SPLIT) && DH == 128 ? 2 : 3) void attn_columns_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
+__global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attn_columns_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
                                                               const int4* __restrict__ items, const int32_t* __restrict__ count,
                                                               const int32_t* __restrict__ block_tables, int max_pages_per_seq,
                                                               float* __restrict__ part_o, float* __restrict__ part_ml,
@@ -647,7 +653,8 @@ __global__ __launch_bounds__(256, (KV8 || SPLIT) && DH == 128 ? 2 : 3) void attn
 // out for the same columns.  A block of 64 tokens of K and V^T is staged in LDS, double buffered and swizzled,
 // and feeds the 32x32x16 MFMAs of all columns; scores are formed transposed, with their rows permuted so that a lane's elements are the
 // consecutive tokens that it supplies to O^T += V^T P^T, as in the prefill kernel, whose masks are not needed here: a prefix is whole pages.
-// Bound: reading the pages up to about a hundred columns, MFMA beyond.
+// Bound: reading the pages up to about a hundred columns, MFMA beyond (and storing the partials: 512 rows of 64 heads behind 1664 tokens, 27.9
+// GFLOP and 34 MB of partials, 48 us).
 template <int DH, int NWC, bool KV8>
 __global__ __launch_bounds__(256, 2) void attn_prefix_kernel(const bf16* __restrict__ q, int64_t ld, int n_q_heads, KvLayout kv,
                                                                             const int4* __restrict__ items, const int32_t* __restrict__ count,

@@ -83,7 +83,9 @@ __device__ __forceinline__ double wave_sum_double(double v) {
 }
 
 // KEEP: a thread has eight vectors at most and keeps them in registers; else the piece is read twice, and the tokens of threads whose
-// largest logit is among the wanted a third time.
+// largest logit is among the wanted a third time.  Bound: reading, 512 rows of 32000 fp32 logits 18.5 us (65.5 MB, 3.5 TB/s with the beginning and
+// the end of two workgroups a CU), 528 of 152067 in bf16, a quarter of them finished, 34 us (120 MB, 3.5 TB/s): beside it a maximum, an exponential and a
+// comparison to a logit.
 template <typename T, bool KEEP>
 __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restrict__ logits, int64_t ld, int shift, const BeamArgs a) {
   __shared__ RowShared rs;
@@ -229,11 +231,11 @@ __device__ __forceinline__ double score_of(u64 order) {
   return __longlong_as_double((long long)(order ^ (order >> 63 ? 1ull << 63 : ~0ull)));
 }
 
-// One workgroup per group, of 256 threads (64 candidates at most) or 1024.  `lists` = beams * pieces lists of k candidates, each in order.  Up to kAllRanked of them are
-// all ranked at once.  Otherwise the first `heads` of every list, n_out in all or more, give a bound, the n_out-th best of them: a
-// list goes on behind its heads only if all of them reach it, so at most n_out / heads lists do, and n_out * k / heads <= 1024 candidates reach
-// it, a few dozen as a rule.
-// Bound: look-ups that wait for each other (three) and barriers.
+// One workgroup per group, of 256 threads (64 candidates at most) or 1024.  `lists` = beams * pieces lists of k candidates, each in order.  Up to
+// kAllRanked of them are all ranked at once.  Otherwise the first `heads` of every list, n_out in all or more, give a bound, the n_out-th best
+// of them: a list goes on behind its heads only if all of them reach it, so at most n_out / heads lists do, and n_out * k / heads <= 1024
+// candidates reach it, a few dozen as a rule.
+// Bound: look-ups that wait for each other (three) and barriers: 16 candidates 4 us, 64 groups of 128 5 us, 33 of 1280 8 us.
 constexpr int kAllRanked = 256;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void beams_group_kernel(const BeamArgs a) {

@@ -121,7 +121,7 @@ constexpr int kCopies = 1 << 30;
 __device__ __forceinline__ int parent_of(const ForkArgs& a, int r) { return a.parents ? a.parents[r] : r < a.n_src ? r : -1; }
 
 // Workgroup 0 looks at the rows, the others at 4096 pages each.  Nothing that the second kernel needs is read from refs again,
-// so that it may change them in place.
+// so that it may change them in place.  Bound: launching, and loads that wait for each other: 3 us of 4 rows, 4 us of 512 rows and 8192 pages.
 __global__ __launch_bounds__(1024) void pages_survey_kernel(const ForkArgs a) {
   __shared__ int part[16];
   __shared__ int bad;
@@ -202,7 +202,8 @@ __global__ __launch_bounds__(1024) void pages_survey_kernel(const ForkArgs a) {
   }
 }
 
-// Workgroup i makes new row i and settles the references of old row i.
+// Workgroup i makes new row i and settles the references of old row i.  Bound: loads that wait for each other (the chunks' counts, the parent,
+// its entries, their references): 3.5 us of 4 rows, 5 to 7.5 us of 512 rows of up to 90 pages.
 __global__ __launch_bounds__(256) void pages_fork_kernel(const ForkArgs a) {
   __shared__ int before[kChunksMost + 1], part[4];
   const int tid = threadIdx.x, wave = tid >> 6, i = blockIdx.x;
@@ -256,6 +257,10 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(const ForkArgs a) {
 }
 
 // ---- compact ---------------------------------------------------------------------------------------------------------------------
+//
+// Five launches, each for what the whole of the one in front of it has to have found: how often the rows name a page; which pages are free, which
+// only the rows hold; their order; the moves; the tables.  Of 5 rows 2.3, 2.2, 4.8, 3.5 and 2.2 us, of 256 rows 2.9, 4.5, 6.9, 5.1 and 2.4: launches
+// and loads that wait for each other, with nothing that takes bandwidth before the copies.
 
 struct CompactArgs {
   const int32_t *src_tables, *lens;
