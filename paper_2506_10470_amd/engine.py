@@ -301,7 +301,7 @@ class BeamSearch:
                                status[step + 1], self.stream)
             for st in self.stages:
                 tdp.tdp_stage_kv_copy_pages(st, copies, rows, self.stream)
-            if (step + 1) % stop_every == 0 and bool((status[:step + 2, :2] != 0).any() | (ended[step] != 0).all()):
+            if (step + 1) % stop_every == 0 and bool((status[:, :2] != 0).any() | (ended[step] != 0).all()):
                 break
             ctx = new_lens - 1
             tdp.tdp_embed_tokens(self.ends, tokens[step], rows, x, self.stream)
@@ -313,7 +313,7 @@ class BeamSearch:
             tdp.tdp_beams_select(self.select, logits, tdp.F32, n, beams, self.vocab_size, self.vocab_size, scores[step % 2],
                                  ended[step - 1] if end_token >= 0 else None, end_token, beams, parents[step], tokens[step], scores[(step + 1) % 2],
                                  ended[step], self.stream)
-        if bool((status[:step + 1, :2] != 0).any()):
+        if bool((status[:, :2] != 0).any()):  # (the fork that ended the search among them)
             raise OutOfPages("a fork of the block tables found no page")
         parents, tokens, final = parents[:step + 1].cpu().tolist(), tokens[:step + 1].cpu().tolist(), scores[(step + 1) % 2].cpu().tolist()
         answers = []

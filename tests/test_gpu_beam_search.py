@@ -153,3 +153,14 @@ def test_refusals():
             with pytest.raises(OutOfPages):
                 search.generate([[1] * 20, [2] * 20], 2, 40)
             assert len(search.generate([[1] * 20], 1, 16)[0]) == 1
+
+
+@pytest.mark.parametrize("stop_every", [1, 3, 100])
+def test_a_fork_that_finds_no_page_is_an_error(stop_every):
+    """Also where it is the one that ends the search.  (generate() asks for enough pages beforehand; what is behind that check is called here.)"""
+    sh = W.SHAPES["tiny"]
+    with Stage(tdp, sh, 16, 4, 40, 2, 4) as st, Ends(sh, VOCAB, 40) as ends:
+        with BeamSearch(tdp, st.h, ends.h, sh.d_model, VOCAB, 5, 4, 4, 40, 2) as search:
+            with pytest.raises(OutOfPages):     # four beams behind 31 tokens: the prompt's two pages, and three more where four are needed
+                search._generate([[1] * 31], 4, 6, -1, stop_every)
+            assert len(search._generate([[1] * 20], 1, 6, -1, stop_every)[0]) == 1
