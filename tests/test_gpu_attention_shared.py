@@ -239,6 +239,26 @@ def test_a_span_of_more_pages_than_a_wave_holds_at_once():
                 assert (out == out[:1]).all()
 
 
+@pytest.mark.parametrize("kv_scales", [None, (0.02, 0.015)])
+@pytest.mark.parametrize("rows", [2, 6, 20])
+def test_pages_behind_more_elements_than_32_bits_count(rows, kv_scales):
+    """The same rows from the first pages of a pool and from the last ones of a pool of over 2^32 elements, where copies have brought them."""
+    heads = (64, 8, 128)
+    with Cache(heads, [(200, [1 + 7 * i for i in range(rows)]), (0, [40])], 16, kv_scales) as c:
+        want, count = c.attend(), (1 << 32) // (8 * 16 * 128) + 500
+        with Stage(tdp, c.stage.shape, count, c.batch, 0, 0, c.width, load_weights=False, kv_scales=kv_scales) as st:
+            for a, b in zip(st.raw_pools(0), c.stage.raw_pools(0)):
+                a.view(-1)[:b.numel()].copy_(b.view(-1))
+            moves = [[p, count - 1 - p] for p in range(c.count)]
+            tdp.tdp_stage_kv_copy_pages(st.h, i32(moves), len(moves))
+            q, out = c.q.cuda(), torch.empty_like(want)
+            tables = i32(np.where(c.tables >= 0, count - 1 - c.tables, -7))
+            tdp.tdp_stage_attend(st.h, 0, q, i32(c.lens), tables, c.batch, i32(c.starts), len(c.starts) - 1, out)
+            torch.cuda.synchronize()
+            c.check(want)
+            assert torch.equal(out, want)
+
+
 def test_infinite_and_missing_numbers_stay_where_they_are():
     """A NaN key or an infinite value in one row's own pages, or in one group's prefix, is nobody else's."""
     with Cache(HEADS["8/2x64"], [(100, [1, 5, 28]), (64, [16, 1]), (80, [3, 3])], 9) as c:

@@ -220,3 +220,57 @@ def test_replayed_on_another_stream():
             graph.replay()
             torch.cuda.synchronize()
             check([parent.cpu().numpy(), token.cpu().numpy(), score.cpu().numpy(), (token == -1).int().cpu().numpy()], z, scores, 4, 8)
+
+
+# ---- the ends of the ranges -----------------------------------------------------------------------------------------
+
+def test_as_many_rows_as_there_may_be():
+    """2048 groups of 32 beams, each the same as its neighbours."""
+    z, s = rows(20, 32, 40)
+    with Beams(1 << 16, 32) as b:
+        got = b.select(z.repeat(2048, 1), s * 2048, 32, 32)
+        for x in got[1:]:
+            assert (x == x[0]).all()
+        assert (got[0] - 32 * np.arange(2048)[:, None] == got[0][0]).all()
+        check([x[:1] for x in got], z, s, 32, 32)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_longest_row(dtype):
+    """2^27 equal logits but for three: the sum is known."""
+    n = 1 << 27
+    z = torch.zeros((1, n), dtype=dtype, device="cuda")
+    z[0, 5], z[0, n - 1], z[0, n // 2 + 1] = 3.0, 4.0, 3.0
+    total = np.log(n - 3 + 2 * np.exp(3.0) + np.exp(4.0))
+    with Beams(1, 5) as b:
+        parent, token, score, _ = b.select(z, [-1.0], 1, 5)
+    assert token.tolist() == [[n - 1, 5, n // 2 + 1, 0, 1]] and (parent == 0).all()
+    want = np.array([4.0, 3.0, 3.0, 0.0, 0.0]) - 1.0 - total
+    assert (np.abs(score[0] - want) <= TOL + 2.0 ** -24 * np.abs(want)).all()
+
+
+def test_rows_further_apart_than_32_bits_count():
+    z, s = rows(21, 4, 3000, torch.bfloat16)
+    far = torch.empty(3 * (1 << 30) + (3 << 4) + 3000, dtype=torch.bfloat16, device="cuda")
+    far = far.as_strided((4, 3000), ((1 << 30) + 16, 1))
+    far.copy_(z)
+    with Beams() as b:
+        for x, y in zip(b.select(far, s, 2, 6), b.select(z, s, 2, 6)):
+            assert np.array_equal(x, y)
+
+
+def test_two_objects_on_two_streams_at_once():
+    inputs = [rows(22 + i, 32, 40000 + i) for i in range(2)]
+    with Beams() as one, Beams() as two:
+        want = [b.select(z, s, 4, 8) for b, (z, s) in zip((one, two), inputs)]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        scores = [torch.tensor(s, device="cuda") for _, s in inputs]
+        outs = [[[torch.empty((8, 8), dtype=t, device="cuda") for t in (torch.int32, torch.int32, torch.float32)] for _ in range(20)] for _ in range(2)]
+        torch.cuda.synchronize()
+        for turn in range(20):
+            for b, (z, _), s, st, out in zip((one, two), inputs, scores, streams, outs):
+                tdp.tdp_beams_select(b.h, z, tdp.F32, 8, 4, z.shape[1], z.shape[1], s, None, -1, 8, *out[turn], None, st)
+        torch.cuda.synchronize()
+        for w, out in zip(want, outs):
+            for got in out:
+                assert all(np.array_equal(a, t.cpu().numpy()) for a, t in zip(w, got))

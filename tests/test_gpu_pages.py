@@ -259,3 +259,43 @@ def test_steps_on_a_side_stream_and_in_a_graph():
             assert (a["t"].tolist(), a["n"].tolist(), a["r"].tolist()) == (tables, lens, refs)
             assert [tuple(c) for c in copies.tolist()] == pairs and tuple(status.tolist()) == st
             parents = [rng.randrange(rows) for _ in range(rows)]
+
+
+# ---- the ends of the ranges -----------------------------------------------------------------------------------------
+
+def test_as_many_rows_and_pages_as_there_may_be():
+    """8192 rows continued and moved in a pool of 2^22 pages, by numpy's account of it."""
+    rng = np.random.default_rng(31)
+    count, n, width = 1 << 22, 8192, 5
+    ids = rng.permutation(count)[:n * 4].astype(np.int32)
+    lens = rng.integers(1, 65, n).astype(np.int32)
+    held = -(-lens // PAGE)
+    tables = np.full((n, width), -1, np.int32)
+    at = np.concatenate([[0], np.cumsum(held)])
+    refs = np.zeros(count, np.int32)
+    for r in range(n):
+        tables[r, :held[r]] = ids[at[r]:at[r + 1]]
+    refs[ids[:at[-1]]] = 1
+    parents = np.arange(n)[::-1].copy()     # every row goes on once: nothing is copied or released
+    with Pages(count, n, width) as pages:
+        got, got_lens, got_refs, copies, status = pages.fork(parents.tolist(), tables.tolist(), lens.tolist(), 16, refs.tolist())
+        fresh = np.nonzero(refs == 0)[0][:n]
+        want = tables[parents].copy()
+        want[np.arange(n), held[parents]] = fresh
+        assert np.array_equal(np.array(got), want) and np.array_equal(got_lens, lens[parents] + 16)
+        assert all(c == (-1, -1) for c in copies) and status == (0, 0, n, count - int((refs > 0).sum()))
+        refs[fresh] = 1
+        assert np.array_equal(got_refs, refs)
+        # one parent for all: its pages are named 8192 times, and all of the others are free again
+        got, got_lens, got_refs, copies, status = pages.fork([7] * n, tables.tolist(), lens.tolist(), 0, (refs * (tables_refs(tables, count) > 0)).tolist())
+        full, rest = int(lens[7]) // PAGE, int(lens[7]) % PAGE
+        named = np.zeros(count, np.int64)
+        np.add.at(named, np.array(got)[np.array(got) >= 0], 1)
+        assert np.array_equal(named, got_refs) and (np.array(got)[:, :full] == tables[7, :full]).all()
+        assert sum(c[0] >= 0 for c in copies) == (n - 1 if rest else 0)
+
+
+def tables_refs(tables, count):
+    refs = np.zeros(count, np.int64)
+    np.add.at(refs, tables[tables >= 0], 1)
+    return refs
