@@ -24,8 +24,8 @@ constexpr int kResident = 3 * 256;  // workgroups of the sixteen-column kernel t
 // 48 / 53 / 55, 64 56 / 55 / 56, 96 59 / 63 / 58, 128 63 / 64 / 59, 512 138 / 114 / 106; 8-bit pools 32 47 / 45 / 45, 48 51 / 47 / 49, 64 60 / 49 /
 // 51; 64 groups of 32 152 / 172 / 182, of 48 203 / 183 / 197.
 // wanted: spans of the prefixes per K/V head (spans of a group times its tiles), as many as make the workgroups that the chip holds at once,
-// twice that for 64 columns.  16 columns, 512 / 768 / 1536 / 3072 workgroups: 8 groups of 8000 tokens, 32 heads 153 / 151 / 155 / 166 us, 32 of 1500
-// 135 / 135 / 141 / 148; 128 columns, 512 rows behind one prompt of 2100, 256 / 512 / 768 / 1536: 157 / 143 / 156 / 170.
+// twice that for 64 columns.  16 columns, 512 / 768 / 1536 / 2048 workgroups: 8 groups of 8000 tokens, 32 heads 153 / 151 / 155 / 161 us, 32 of 1500
+// 135 / 135 / 141 / 143; 128 columns, 512 rows behind one prompt of 2100, 256 / 512 / 768 / 1536: 157 / 143 / 156 / 170.
 struct Form {
   int columns, wanted;
 };
