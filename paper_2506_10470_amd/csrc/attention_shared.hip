@@ -15,6 +15,10 @@ namespace tdp {
 namespace {
 
 constexpr int kMinSpanPages = kDecodeSpanMin / 16;
+// Partials that one wave of four joins by itself, one after another; of more each has a quarter, four on their way at a time.  Whole calls, 8
+// K/V heads, never / from 8 / from 24 on: a row of 4000 tokens 30 / 27 / 30 us, 4 rows of up to 8000 46 / 50 / 46 and of up to 16000 95 / 83 / 83, a row
+// of up to 32000 70 / 54, of up to 131000 164 / 124; two rows behind a prefix of 131000, 2 heads, 174 / 112.
+constexpr int kJoinedAlone = 8;
 constexpr int kResident = 3 * 256;  // workgroups of the sixteen-column kernel that the chip holds at once (two to three per CU)
 
 // How a batch is attended to: a pure function of sizes that the host knows.
@@ -326,6 +330,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attn_columns_kernel(co
   constexpr int kChunk = 256;        // pages whose ids the wave holds at once, four to a lane
   constexpr int PITCH = DT * 4 + 2;
   __shared__ float s_state[SPLIT ? 3 * 64 * PITCH : 1];
+  __shared__ int s_last;
   const int Hkv = kv.n_kv_heads, G = n_q_heads / Hkv;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, kg = lane >> 4;
@@ -547,8 +552,9 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attn_columns_kernel(co
         o[d] = o[d] * mine + x * its;
       }
     };
-    if constexpr (SPLIT) {  // the other waves' states, in order
-      __syncthreads();  // (of the unit before have been read)
+    // the other waves' states, in order, joined by the first wave
+    auto gather = [&] {
+      __syncthreads();  // (those of before have been read)
       if (wave > 0) {
         float* const at = s_state + ((wave - 1) * 64 + lane) * PITCH;
 #pragma unroll
@@ -558,7 +564,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attn_columns_kernel(co
         *reinterpret_cast<float2*>(at + DT * 4) = make_float2(m, lsum);
       }
       __syncthreads();
-      if (wave > 0) continue;
+      if (wave > 0) return;
 #pragma unroll
       for (int w = 0; w < 3; ++w) {
         const float* const at = s_state + (w * 64 + lane) * PITCH;
@@ -568,6 +574,10 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attn_columns_kernel(co
           return f32x4{x.x, x.y, y.x, y.y};
         });
       }
+    };
+    if constexpr (SPLIT) {
+      gather();
+      if (PREFIX && wave > 0) continue;
     }
     // (the item is read again: what it says would hold registers through all of the above)
     int item_again = item;
@@ -587,42 +597,81 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attn_columns_kernel(co
         if (kg == 0) *reinterpret_cast<float2*>(part_ml + (base + slot) * 2) = make_float2(m, lsum);
       }
     } else {
+      // The waves share the joining out as well where there is much of it.
+      const bool together = SPLIT && in_front + own_spans > kJoinedAlone;
+      if (SPLIT && wave > 0 && !together) continue;
       if (own_spans > 1) {
         // The spans of a row are made on different XCDs, whose L2s do not see each other: partials are stored and read past them, the wave waits
         // until its stores have arrived, and only then is the span counted.  The last one puts the counter back for the next launch.
-        if (real) {
+        bool last = false;
+        if (!SPLIT || wave == 0) {
+          if (real) {
 #pragma unroll
-          for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) store_agent(o_at + (int64_t)slot * DH + d * 16 + i, o[d][i]);
-          if (kg == 0) {
-            store_agent(part_ml + (base + slot) * 2, m);
-            store_agent(part_ml + (base + slot) * 2 + 1, lsum);
+              for (int i = 0; i < 4; ++i) store_agent(o_at + (int64_t)slot * DH + d * 16 + i, o[d][i]);
+            if (kg == 0) {
+              store_agent(part_ml + (base + slot) * 2, m);
+              store_agent(part_ml + (base + slot) * 2 + 1, lsum);
+            }
           }
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          unsigned before = 0;
+          unsigned* const done = spans_done + (int64_t)row * Hkv + kvh;
+          if (lane == 0) before = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          before = __builtin_amdgcn_readfirstlane(before);
+          last = before + 1 == (unsigned)own_spans;
+          if (last && lane == 0) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        unsigned before = 0;
-        unsigned* const done = spans_done + (int64_t)row * Hkv + kvh;
-        if (lane == 0) before = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        before = __builtin_amdgcn_readfirstlane(before);
-        if (before + 1 != (unsigned)own_spans) continue;
-        if (lane == 0) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (together) {
+          if (threadIdx.x == 0) s_last = last;  // (that of the unit before was read in front of a barrier)
+          __syncthreads();
+          last = s_last;
+        }
+        if (!last) continue;
+      }
+      if (own_spans > 1 || (SPLIT && wave > 0)) {
         m = kNegBig;
         lsum = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
       // in the order of the spans, whoever is last (a row's only span, in registers, first)
-      for (int k = 0; k < in_front; ++k) {
-        const float* const from = o_at + (int64_t)k * DH;
-        const float2 ml = *reinterpret_cast<const float2*>(part_ml + (base + k) * 2);
-        f32x4 x[DT];
+      const int all = in_front + (own_spans > 1 ? own_spans : 0);
+      if (together) {
+        // a quarter to a wave, four on their way at a time
+        const int from_k = (wave * all) >> 2, to_k = ((wave + 1) * all) >> 2;
+        for (int k = from_k; k < to_k; k += 4) {
+          float2 ml[4];
+          float2 x[4][2 * DT];
 #pragma unroll
-        for (int d = 0; d < DT; ++d) x[d] = *reinterpret_cast<const f32x4*>(from + d * 16);
-        join(ml.x, ml.y, [&](int d) { return x[d]; });
-      }
-      if (own_spans > 1)
-        for (int k = in_front; k < in_front + own_spans; ++k) {
+          for (int u = 0; u < 4; ++u) {
+            const int at = min(k + u, to_k - 1);
+            const float* const from = o_at + (int64_t)at * DH;
+            ml[u] = load_agent2(part_ml + (base + at) * 2);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              x[u][2 * d] = load_agent2(from + d * 16);
+              x[u][2 * d + 1] = load_agent2(from + d * 16 + 2);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (k + u < to_k)
+              join(ml[u].x, ml[u].y, [&](int d) { return f32x4{x[u][2 * d].x, x[u][2 * d].y, x[u][2 * d + 1].x, x[u][2 * d + 1].y}; });
+        }
+        gather();
+        if (wave > 0) continue;
+      } else {
+        for (int k = 0; k < in_front; ++k) {
+          const float* const from = o_at + (int64_t)k * DH;
+          const float2 ml = *reinterpret_cast<const float2*>(part_ml + (base + k) * 2);
+          f32x4 x[DT];
+#pragma unroll
+          for (int d = 0; d < DT; ++d) x[d] = *reinterpret_cast<const f32x4*>(from + d * 16);
+          join(ml.x, ml.y, [&](int d) { return x[d]; });
+        }
+        for (int k = in_front; k < all; ++k) {
           const float* const from = o_at + (int64_t)k * DH;
           const float2 ml = load_agent2(part_ml + (base + k) * 2);
           f32x4 x[DT];
@@ -633,6 +682,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 2 : 3) void attn_columns_kernel(co
           }
           join(ml.x, ml.y, [&](int d) { return x[d]; });
         }
+      }
       if (real) {
         const float scale = it.z > 0 ? out_scale / lsum : 0.f;  // (a row without tokens gives zeros)
 #pragma unroll

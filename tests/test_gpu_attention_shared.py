@@ -147,6 +147,18 @@ def test_rows_of_several_spans_behind_a_prefix(heads, span):
         c.check(c.attend())
 
 
+@pytest.mark.parametrize("kv_scales", [None, (0.02, 0.015)])
+@pytest.mark.parametrize("heads", ["8/2x64", "6/3x128"])
+def test_partials_that_the_waves_share_out(heads, kv_scales):
+    """Rows of up to forty spans, behind prefixes of none, of few and of many; the same bits again."""
+    for groups in ([(0, [1800, 2100, 2400, 10000])], [(600, [1, 1500, 1800, 5000, 300])], [(9000, [1, 20, 300, 700])], [(2048, [1, 256, 257, 16])]):
+        with Cache(HEADS[heads], groups, 17, kv_scales) as c:
+            tdp.tdp_stage_set_decode_span(c.stage.h, 256)
+            out = c.attend()
+            c.check(out)
+            assert all(torch.equal(out, c.attend()) for _ in range(5))
+
+
 def test_rows_that_fill_their_tables():
     """Spans of the prefix and of the rows together are no more than a row has slots for."""
     for prefix, width in ((16, 16), (16, 33), (256, 32), (272, 33), (1008, 64), (496, 48)):
