@@ -65,7 +65,10 @@ constexpr int kPlanThreads = 256, kPlanRows = 16;  // rows that a workgroup comp
 constexpr int kPlanHeld = 1024;                    // rows, and groups, that the last workgroup holds in LDS
 constexpr int kClasses = 17;                       // of row spans by their length
 typedef i32x4 __attribute__((aligned(4))) i32x4_of_int;
-__device__ __forceinline__ int row_tokens(const SharedBatch& b, int r) { return min(max(b.lens[r], 0) + b.add, b.max_pages_per_seq * 16); }
+// (The length is brought into the row's range before `add` joins it, as a decode step brings its position: 2^31 - 1 + 1 would be no length.)
+__device__ __forceinline__ int row_tokens(const SharedBatch& b, int r) {
+  return min(max(b.lens[r], 0), b.max_pages_per_seq * 16 - b.add) + b.add;
+}
 
 // A thread's value plus those of all threads of the workgroup in front of it, and the sum of all.
 __device__ __forceinline__ int plan_scan(int v, int* part, int* total) {
