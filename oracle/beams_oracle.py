@@ -9,7 +9,8 @@ def candidates(logits: np.ndarray, scores: np.ndarray, finished, end_token: int)
     z = np.asarray(logits, np.float64)
     with np.errstate(all="ignore"):
         top = np.max(z, 1, keepdims=True)                       # (NaN stays)
-        c = np.asarray(scores, np.float64)[:, None] + (z - (top + np.log(np.exp(z - top).sum(1, keepdims=True))))
+        # (the logarithm joins the distance to the largest, not the largest: beside -3e38 it would be lost)
+        c = np.asarray(scores, np.float64)[:, None] + ((z - top) - np.log(np.exp(z - top).sum(1, keepdims=True)))
     if finished is not None:
         done = np.asarray(finished) != 0
         c[done] = -np.inf

@@ -5,11 +5,13 @@
 // the logits, so nothing else of the row can be chosen.  The second has a workgroup to a group: it joins the sums of every row and ranks the
 // candidates of all beams.
 //
-// Scores of different beams are often close, and which token goes on depends on their order, so what is compared is in 64 bits.  The
-// exponentials are in fp32, e^(z - r) = 2^(z log2 e - R) for an R near r log2 e: log2 e in two parts, a fused multiply-add each, so that the
-// exponent is rounded by 2^-24 of itself and nothing large cancels; what is summed is relative to R itself, and the logarithm joins it
-// again in 64 bits.  What is left, the instruction's own error (1 ulp, in no order) and the rounding of a thread's sum, averages out to
-// below 1e-8 of a sum of thousands of terms.
+// Scores of different beams are often close, and which token goes on depends on their order, so what is compared is in 64 bits.  Only the
+// exponentials are formed in fp32: relative to the largest logit m of the piece, t = z - m and e^t = 2^(t log2 e) with log2 e in two parts.  The
+// largest logit's own term is 1 and nothing else (a row held to one token costs exactly nothing), and rows that differ by a constant have
+// the same t, the same sums and the same costs to the bit.  Of any other term t and the exponent are rounded by 2^-24 of themselves, each |t| 2^-24 of
+// the term, and the instruction's error is 1 ulp: (1 + |t|) 2^-23 in all.  Terms are added in 64 bits, so ln sum is off by at most
+//   2^-23 sum_{z < m} p (1 + m - z),     p the tokens' probabilities:
+// nothing of what the likeliest token carries.  (Errors of many different logits largely cancel; those of equal logits are equal.)
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -44,8 +46,7 @@ struct BeamArgs {
   const float* scores;
   // per (row, piece)
   float* max;
-  double* reference;  // R ln 2
-  double* sum;
+  double* sum;  // relative to it
   u64* keys;  // [k], in order, 0 behind the last
   int32_t *parent, *token;
   float* score;
@@ -53,9 +54,10 @@ struct BeamArgs {
 };
 
 constexpr float kLog2High = 1.44269502f, kLog2Low = 1.92596299e-8f;  // log2 e
-// 2^(z log2 e - R)
-__device__ __forceinline__ float exp_from(float z, float R) {
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2Low, __builtin_fmaf(z, kLog2High, -R)));
+// e^(z - m), 1 where they are equal
+__device__ __forceinline__ float exp_below(float z, float m) {
+  const float t = z - m;
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(t, kLog2High, t * kLog2Low));
 }
 
 // A piece of a row in vectors from its first element on, wherever that lies in memory: which terms a thread adds up, and with them
@@ -83,9 +85,10 @@ __device__ __forceinline__ double wave_sum_double(double v) {
 }
 
 // KEEP: a thread has eight vectors at most and keeps them in registers; else the piece is read twice, and the tokens of threads whose
-// largest logit is among the wanted a third time.  Bound: reading, 512 rows of 32000 fp32 logits 18.5 us (65.5 MB, 3.5 TB/s with the beginning and
-// the end of two workgroups a CU), 528 of 152067 in bf16, a quarter of them finished, 34 us (120 MB, 3.5 TB/s): beside it a maximum, an exponential and a
-// comparison to a logit.
+// largest logit is among the wanted a third time.  Bound: reading, 512 rows of 32000 fp32 logits 18.3 us (65.5 MB, 3.6 TB/s with the beginning and
+// the end of two workgroups a CU), 528 of 152067 in bf16, a quarter of them finished, 39 us (120 MB, 3.1 TB/s): beside it a maximum, an exponential, an
+// addition in 64 bits and a comparison to a logit.  (Terms added in fp32 per thread 17.9 and 36 us, in pairs 18.2 and 38; a sum so formed
+// is off by 2^-24 of what the likeliest token carries.)
 template <typename T, bool KEEP>
 __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restrict__ logits, int64_t ld, int shift, const BeamArgs a) {
   __shared__ RowShared rs;
@@ -100,7 +103,6 @@ __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restric
     for (int i = tid; i < a.k; i += threads) keys[i] = piece == 0 && i == 0 ? key_of(0.f, a.end_token) : 0;
     if (tid == 0) {
       a.max[slot] = piece == 0 ? 0.f : -INFINITY;
-      a.reference[slot] = 0.0;
       a.sum[slot] = piece == 0 ? 1.0 : 0.0;
     }
     return;
@@ -155,26 +157,17 @@ __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restric
   __syncthreads();
   float max = rs.wave_max[0];
   for (int w = 1; w < waves; ++w) max = fmaxf(max, rs.wave_max[w]);
-  // Sums relative to it (to 0 where nothing is above minus infinity): a few terms in fp32, the rest in 64 bits.  Logits whose multiple of
-  // log2 e could overflow are taken relative to the maximum first.
-  const float r = max == -INFINITY ? 0.f : max, shift_by = fabsf(r) > 1e37f ? r : 0.f;
-  const float R = (r - shift_by) * kLog2High;
-  double total = edge_at >= 0 ? (double)exp_from(edge - shift_by, R) : 0.0;
+  // Sums relative to it (to 0 where nothing is above minus infinity).
+  const float r = max == -INFINITY ? 0.f : max;
+  double total = edge_at >= 0 ? (double)exp_below(edge, r) : 0.0;
   auto add = [&](int v0) {
-    float sum = 0.f;
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
       if (u > 0 && v0 - tid + u * threads >= row.body) break;  // (the same for all threads)
       asm volatile("" : "+v"(z[u]));  // (bf16: converted here again, the values of two passes would not fit)
-      if (shift_by == 0.f) {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) sum += exp_from(Values::value(z[u], e), R);
-      } else {
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) sum += exp_from(Values::value(z[u], e) - shift_by, R);
-      }
+      for (int e = 0; e < kPer; ++e) total += (double)exp_below(Values::value(z[u], e), r);
     }
-    total += (double)sum;
   };
   if constexpr (KEEP) {
     add(tid);
@@ -191,7 +184,6 @@ __global__ __launch_bounds__(1024, 8) void beams_piece_kernel(const T* __restric
   if (tid == 0) {
     for (int w = 1; w < waves; ++w) total += wave_total[w];
     a.max[slot] = max;
-    a.reference[slot] = (double)shift_by + (double)R * 0.69314718055994530942;
     a.sum[slot] = total;
   }
   const int found = select_top(
@@ -239,7 +231,7 @@ __device__ __forceinline__ double score_of(u64 order) {
 constexpr int kAllRanked = 256;
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void beams_group_kernel(const BeamArgs a) {
-  __shared__ double log_total[TDP_MAX_BEAMS];
+  __shared__ double largest[TDP_MAX_BEAMS], log_total[TDP_MAX_BEAMS];  // of a row's logits; of its sum relative to that
   __shared__ Candidate pool[kListsMost];
   __shared__ Candidate bound;
   __shared__ int count, places[kListsMost];
@@ -252,15 +244,15 @@ __global__ __launch_bounds__(THREADS) void beams_group_kernel(const BeamArgs a) 
     const bool in = lane < a.pieces;
     const int64_t slot = slot0 + b * a.pieces + lane;
     const float own = in ? a.max[slot] : -INFINITY;
-    const double at = in ? a.reference[slot] : 0.0, sum = in ? a.sum[slot] : 0.0;
-    // relative to the reference of the piece with the largest logit
+    const double sum = in ? a.sum[slot] : 0.0;
     float max = own;
     for (int o = 1; o < 64; o *= 2) max = fmaxf(max, __shfl_xor(max, o, 64));
-    const int of = __ffsll((long long)__ballot(own == max)) - 1;
-    const double reference = __shfl(at, of, 64);
     // (of a piece with nothing but minus infinity and NaN the sum alone counts: 0, or NaN)
-    const double total = wave_sum_double(own == -INFINITY ? sum : sum * exp(at - reference));
-    if (lane == 0) log_total[b] = max == -INFINITY ? NAN : reference + log(total);
+    const double total = wave_sum_double(own == -INFINITY ? sum : sum * exp((double)own - (double)max));
+    if (lane == 0) {
+      largest[b] = (double)max;
+      log_total[b] = max == -INFINITY ? NAN : log(total);
+    }
   }
   if (tid == 0) {
     bound = Candidate{0, 0};
@@ -271,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void beams_group_kernel(const BeamArgs a) 
   auto candidate = [&](u64 key, float score, int beam) {
     if (!key) return Candidate{0, 0};
     const unsigned order = (unsigned)(key >> 32);
-    const double c = (double)score + ((double)logit_of(order) - log_total[beam]);
+    const double c = (double)score + (((double)logit_of(order) - largest[beam]) - log_total[beam]);
     if (!(c > -INFINITY)) return Candidate{0, 0};
     const long long bits = __double_as_longlong(c + 0.0);
     return Candidate{(u64)bits ^ (bits < 0 ? ~0ull : 1ull << 63),
@@ -370,7 +362,7 @@ struct tdp_beams {
   tdp_beams_config cfg;
   int device = 0;
   float* max = nullptr;
-  double* sum = nullptr;  // and the references behind them
+  double* sum = nullptr;
   u64* keys = nullptr;
 };
 
@@ -388,7 +380,7 @@ int tdp_beams_create(const tdp_beams_config* cfg, tdp_beams** out) {
   h->device = dev;
   const size_t slots = slots_of(cfg->max_rows);
   hipError_t e = hipMalloc((void**)&h->max, slots * sizeof(float));
-  if (e == hipSuccess) e = hipMalloc((void**)&h->sum, 2 * slots * sizeof(double));
+  if (e == hipSuccess) e = hipMalloc((void**)&h->sum, slots * sizeof(double));
   if (e == hipSuccess) e = hipMalloc((void**)&h->keys, slots * cfg->max_out * sizeof(u64));
   if (e != hipSuccess) {
     const int code = fail_hip(e, "tdp_beams_create");
@@ -433,8 +425,7 @@ int tdp_beams_select(tdp_beams* h, const void* logits, int32_t dtype, int32_t n_
   const bool keep = vectors <= threads * kInFlight;
   int shift = 0;  // of the elements that a thread has read
   while ((1 << shift) < (vectors + threads - 1) / threads * per) ++shift;
-  const size_t slots = slots_of(h->cfg.max_rows);
-  const BeamArgs a{beams, n, width, used, n_out, finished, end_token, scores, h->max, h->sum + slots, h->sum, h->keys, parent, token, score, finished_out};
+  const BeamArgs a{beams, n, width, used, n_out, finished, end_token, scores, h->max, h->sum, h->keys, parent, token, score, finished_out};
   const unsigned grid = (unsigned)rows * used;
   const size_t lds = keep ? threads / 64 * sizeof(StagedUnits) : 0;
 #define TDP_PIECES(T, KEEP) beams_piece_kernel<T, KEEP><<<grid, threads, lds, s>>>((const T*)logits, ld, shift, a)
