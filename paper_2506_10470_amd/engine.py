@@ -222,8 +222,12 @@ class BeamSearch:
                              else torch.cuda.ExternalStream(getattr(self.stream, "cuda_stream", self.stream)))
         rows = max(max_batch, max_seqs, 1)
         self.pages = self.select = None
-        self.pages = tdp.tdp_pages_create(tdp.PagesConfig(num_pages, rows, max_pages_per_seq))
-        self.select = tdp.tdp_beams_create(tdp.BeamsConfig(rows, tdp.MAX_TOP))
+        try:
+            self.pages = tdp.tdp_pages_create(tdp.PagesConfig(num_pages, rows, max_pages_per_seq))
+            self.select = tdp.tdp_beams_create(tdp.BeamsConfig(rows, tdp.MAX_TOP))
+        except BaseException:
+            self.close()
+            raise
 
     def close(self) -> None:
         """Gives the library's objects back."""
@@ -242,7 +246,8 @@ class BeamSearch:
     def generate(self, prompts: Sequence[Sequence[int]], beams: int, max_new: int, end_token: int = -1,
                  stop_every: int = 8) -> List[List[Tuple[List[int], float]]]:
         """For every prompt its beams, best first: (generated tokens, sum of their log-probabilities).  A beam that chose end_token keeps it as
-        its last token.  Beams that never had a continuation of their own (a vocabulary smaller than the beams) are left out."""
+        its last token.  Beams that never had a continuation of their own (logits without a distribution, or with fewer tokens above minus infinity
+        than beams) are left out."""
         n = len(prompts)
         if n < 1 or any(len(p) < 1 for p in prompts):
             raise ValueError("every prompt needs a token")
