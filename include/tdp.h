@@ -465,7 +465,7 @@ TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_r
  * the row's largest logit m: its own is exactly 1 (a row held to one token costs nothing), and ln sum is off by at most
  * 2^-23 sum_{z < m} p (1 + m - z), p the tokens' probabilities.
  *   logits   dev, TDP_F32 or TDP_BF16, [n_groups * beams][n], rows ld >= n elements apart, at any alignment of their type
- *   scores   dev fp32 [n_groups * beams], not overlapping score
+ *   scores   dev fp32 [n_groups * beams]; the results overlap neither them nor one another (finished_out may be finished itself)
  *   finished dev int32 [n_groups * beams], not 0: finished; or null.  end_token: in [0, n), or, with finished null, -1: none
  * beams 1 .. TDP_MAX_BEAMS, n_out 1 .. TDP_MAX_TOP and at most beams * n, n up to 2^27, n_groups * beams <= max_rows (0: nothing to do).
  * A tdp_beams owns scratch.  It lives on the device that is current when it is created, calls on it need that device current, and it must
@@ -499,7 +499,8 @@ TDP_API int tdp_beams_select(tdp_beams* h, const void* logits, int32_t dtype, in
  * n_src = 0 makes new rows alone, n_dst = 0 releases all.  Page ids in src_tables are trusted as everywhere; reference counts of ids
  * outside the pool are skipped.
  *   parents, add, dst_lens dev int32 [n_dst]; copies dev int32 [n_dst][2]; src_lens dev int32 [n_src]; src_tables, dst_tables
- *   dev int32 [n_src], [n_dst] [max_pages_per_seq], not overlapping; refs_in, refs_out dev int32 [num_pages] */
+ *   dev int32 [n_src], [n_dst] [max_pages_per_seq]; refs_in, refs_out dev int32 [num_pages].  But for refs_out, no output overlaps an input or
+ *   another output. */
 typedef struct tdp_pages tdp_pages;
 typedef struct {
   int32_t num_pages;          /* 1 .. 2^22 */
@@ -515,7 +516,8 @@ TDP_API int tdp_pages_fork(tdp_pages* h, const int32_t* parents, const int32_t* 
  * lowest free one, as long as that is lower.  Movable are pages that the n_rows given rows name and nobody else holds (refs equal to
  * the entries that name them); others stay.  dst_tables (may be src_tables itself) are the rows with the new ids, -1 behind a row's pages,
  * moves (dev int32 [max_moves][2]) the (old, new) ids for tdp_stage_kv_copy_pages, (-1, -1) behind the last.  status: 0, rows that are
- * refused (a length out of range, an id outside the pool; nothing moves then), moves, pages in use.  max_moves 1 .. 2^22. */
+ * refused (a length out of range, an id outside the pool; nothing moves then), moves, pages in use.  max_moves 1 .. 2^22.  refs_out may be
+ * refs_in itself; apart from these two no output overlaps an input or another output. */
 TDP_API int tdp_pages_compact(tdp_pages* h, const int32_t* src_tables, const int32_t* lens, int32_t n_rows, int32_t max_moves,
                               const int32_t* refs_in, int32_t* refs_out, int32_t* dst_tables, int32_t* moves, int32_t* status,
                               void* stream);

@@ -413,6 +413,10 @@ int tdp_beams_select(tdp_beams* h, const void* logits, int32_t dtype, int32_t n_
   if (n_groups == 0) return TDP_OK;
   if (!logits || !scores || !parent || !token || !score) return probe_fail(TDP_EINVAL, "null pointer");
   if ((uintptr_t)logits & (dtype == TDP_F32 ? 3 : 1)) return probe_fail(TDP_EINVAL, "logits must be aligned to their type");
+  // (scores are read while results of other groups are written; everything else is read in front of them)
+  const int64_t results = 4ll * n_groups * n_out;
+  const Range in[] = {{scores, 4ll * n_groups * beams}}, out[] = {{parent, results}, {token, results}, {score, results}, {finished_out, results}};
+  if (any_meet(in, out)) return probe_fail(TDP_EINVAL, "outputs must not overlap the scores or one another");
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return fail_hip(e, "hipGetDevice");

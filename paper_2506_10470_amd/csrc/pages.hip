@@ -403,11 +403,6 @@ int fail_hip(hipError_t e, const char* what) {
   return probe_fail(e == hipErrorOutOfMemory ? TDP_ENOMEM : TDP_EHIP, buf);
 }
 
-bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
-}
-
 }  // namespace
 
 hipError_t launch_kv_copy_pages(const KvLayout& kv, int64_t layer_bytes, int n_layers, const int32_t* pairs, int n, hipStream_t s) {
@@ -493,9 +488,10 @@ int tdp_pages_fork(tdp_pages* h, const int32_t* parents, const int32_t* src_tabl
   if (n_src > 0 && (!src_tables || !src_lens)) return probe_fail(TDP_EINVAL, "null pointer");
   if (n_dst > 0 && (!dst_tables || !dst_lens || !copies)) return probe_fail(TDP_EINVAL, "null pointer");
   const int64_t W = h->cfg.max_pages_per_seq, N = h->cfg.num_pages;
-  if (refs_in != refs_out && overlap(refs_in, 4 * N, refs_out, 4 * N)) return probe_fail(TDP_EINVAL, "refs_out must be refs_in or apart from it");
-  if (n_src > 0 && n_dst > 0 && (overlap(src_tables, 4 * W * n_src, dst_tables, 4 * W * n_dst) || overlap(src_lens, 4ll * n_src, dst_lens, 4ll * n_dst)))
-    return probe_fail(TDP_EINVAL, "the new rows must not overlap the old ones");
+  // (rows are made by workgroups of their own, which read what belongs to others)
+  const Range in[] = {{parents, 4ll * n_dst}, {add, 4ll * n_dst}, {src_lens, 4ll * n_src}, {src_tables, 4 * W * n_src}, {refs_in == refs_out ? nullptr : refs_in, 4 * N}};
+  const Range out[] = {{refs_out, 4 * N}, {dst_tables, 4 * W * n_dst}, {dst_lens, 4ll * n_dst}, {copies, 8ll * n_dst}, {status, 16}};
+  if (any_meet(in, out)) return probe_fail(TDP_EINVAL, "outputs must not overlap inputs or one another (refs_out may be refs_in itself)");
   const int rc = check_pages_device(h);
   if (rc != TDP_OK) return rc;
   hipStream_t s = (hipStream_t)stream;
@@ -517,9 +513,10 @@ int tdp_pages_compact(tdp_pages* h, const int32_t* src_tables, const int32_t* le
   if (!refs_in || !refs_out || !moves || !status) return probe_fail(TDP_EINVAL, "null pointer");
   if (n_rows > 0 && (!src_tables || !lens || !dst_tables)) return probe_fail(TDP_EINVAL, "null pointer");
   const int64_t bytes = 4ll * h->cfg.max_pages_per_seq * n_rows, N = h->cfg.num_pages;
-  if (refs_in != refs_out && overlap(refs_in, 4 * N, refs_out, 4 * N)) return probe_fail(TDP_EINVAL, "refs_out must be refs_in or apart from it");
-  if (src_tables != dst_tables && n_rows > 0 && overlap(src_tables, bytes, dst_tables, bytes))
-    return probe_fail(TDP_EINVAL, "dst_tables must be src_tables or apart from them");
+  const Range in[] = {{src_tables == dst_tables ? nullptr : src_tables, bytes}, {lens, 4ll * n_rows}, {refs_in == refs_out ? nullptr : refs_in, 4 * N}};
+  const Range out[] = {{refs_out, 4 * N}, {dst_tables, bytes}, {moves, 8ll * max_moves}, {status, 16}};
+  if (any_meet(in, out))
+    return probe_fail(TDP_EINVAL, "outputs must not overlap inputs or one another (dst_tables may be src_tables itself, refs_out refs_in)");
   const int rc = check_pages_device(h);
   if (rc != TDP_OK) return rc;
   hipStream_t s = (hipStream_t)stream;

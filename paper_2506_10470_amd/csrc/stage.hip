@@ -660,6 +660,7 @@ int tdp_stage_attend(tdp_stage* st, int32_t layer, const void* q, const int32_t*
   if (batch == 0) return TDP_OK;
   if (!q || !out || !lens || !block_tables) return fail(TDP_EINVAL, "null pointer");
   if (((uintptr_t)q & 15) || ((uintptr_t)out & 7)) return fail(TDP_EINVAL, "q must be 16-byte and out 8-byte aligned");
+  if (Range{q, 2 * st->dq * batch}.meets(Range{out, 2 * st->dq * batch})) return fail(TDP_EINVAL, "out must not overlap q");
   const int rc = check_groups(st, group_starts, n_groups);
   if (rc != TDP_OK) return rc;
   const SharedBatch shared = shared_batch(st, Groups{group_starts, n_groups}, lens, 0, block_tables, batch);

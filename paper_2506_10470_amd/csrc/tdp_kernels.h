@@ -5,6 +5,27 @@
 
 namespace tdp {
 
+// A range of memory that a call reads or writes, for the refusal of arguments that overlap.
+struct Range {
+  const void* at;
+  int64_t bytes;
+  bool meets(const Range& o) const {
+    const uintptr_t x = (uintptr_t)at, y = (uintptr_t)o.at;
+    return at && o.at && bytes > 0 && o.bytes > 0 && x < y + (uintptr_t)o.bytes && y < x + (uintptr_t)bytes;
+  }
+};
+// Whether an output meets an input or another output.
+template <int N_IN, int N_OUT>
+static inline bool any_meet(const Range (&in)[N_IN], const Range (&out)[N_OUT]) {
+  for (int o = 0; o < N_OUT; ++o) {
+    for (int i = 0; i < N_IN; ++i)
+      if (out[o].meets(in[i])) return true;
+    for (int p = 0; p < o; ++p)
+      if (out[o].meets(out[p])) return true;
+  }
+  return false;
+}
+
 // ---- operand layouts -----------------------------------------------------------------------------
 // Element (row r, column k) of a GEMM operand lives at
 //     (r >> shift) * group + (k >> 5) * kb + (r & (2^shift - 1)) * par + (k & 31)
