@@ -6,6 +6,8 @@
 // the groups are.  Three launches: the plan (once per step), the prefixes, the rows.  The prefix kernel leaves partials (reference m, sum
 // l, unnormalised output o, per span of the prefix) in the first slots of every row and head; a row's own kernel attends to what the row has
 // behind its prefix and combines all.
+//
+// Times of whole calls in the comments here are of calls alone, each behind a write that has emptied the caches.
 #include <algorithm>
 
 #include "tdp_device.h"
@@ -23,13 +25,17 @@ constexpr int kResident = 3 * 256;  // workgroups of the sixteen-column kernel t
 
 // How a batch is attended to: a pure function of sizes that the host knows.
 //
-// columns: of a tile of the prefix kernel, by the average group's.  Four groups with a prefix of 2400 to 4000 tokens, 8 K/V heads of 128
-// channels, 8 query heads to each, the whole call, tiles of 16 / 64 / 128 columns: groups of 24 columns 39 / 48 / 49 us, 32 46 / 53 / 54, 48
-// 48 / 53 / 55, 64 56 / 55 / 56, 96 59 / 63 / 58, 128 63 / 64 / 59, 512 138 / 114 / 106; 8-bit pools 32 47 / 45 / 45, 48 51 / 47 / 49, 64 60 / 49 /
-// 51; 64 groups of 32 152 / 172 / 182, of 48 203 / 183 / 197.
+// columns: of a tile of the prefix kernel, by the average group's (a large group among many small ones gets the small ones' tiles and is read once
+// for each).  Prefixes of 1200 to 2000 tokens, 8 K/V heads of 128 channels, 8 query heads to each, the whole call, tiles of 16 / 64 / 128
+// columns: 64 groups of 32 columns 136 / 171 / 180 us, of 48 201 / 185 / 195, of 128 380 / 226 / 225, 16 groups of 96 87 / 93 / 90, of 128 107 / 97 /
+// 96, 24 of 256 216 / 148 / 141.  Of few groups the tiles count less: four with a prefix of 2400 to 4000 tokens, of 24 columns 39 / 48 / 49, 32
+// 44 / 52 / 52, 48 47 / 51 / 52, 64 53 / 55 / 55, 96 57 / 67 / 62, 128 59 / 66 / 62, 256 85 / 99 / 90, 512 137 / 112 / 105; 8-bit pools 24
+// 41 / 41 / 42, 32 44 / 44 / 44, 48 48 / 45 / 47, 64 51 / 48 / 49, 96 53 / 58 / 55, 128 56 / 62 / 58, 256 79 / 93 / 88, 512 107 / 97 / 93 (so with 64 to
+// 256 columns four groups would have up to 15 % from tiles of 16).
 // wanted: spans of the prefixes per K/V head (spans of a group times its tiles), as many as make the workgroups that the chip holds at once,
-// twice that for 64 columns.  16 columns, 512 / 768 / 1536 / 2048 workgroups: 8 groups of 8000 tokens, 32 heads 153 / 151 / 155 / 161 us, 32 of 1500
-// 135 / 135 / 141 / 143; 128 columns, 512 rows behind one prompt of 2100, 256 / 512 / 768 / 1536: 157 / 143 / 156 / 170.
+// twice that for 64 columns.  16 columns, 512 / 768 / 1536 / 2048 workgroups: 8 groups of 8000 tokens, 32 heads 148 / 147 / 148 / 156 us, 32 of 1500
+// 135 / 135 / 141 / 142; 64 columns, 4 groups of 8 x 8, 512 / 768 / 1024 / 1536: 55 / 53 / 53 / 53; 128 columns, 512 rows behind one prompt of 2100,
+// 256 / 512 / 768 / 1536: 155 / 140 / 152 / 166.
 struct Form {
   int columns, wanted;
 };
@@ -43,8 +49,8 @@ Form form_of(int batch, int n_groups, int n_q_heads, int n_kv_heads) {
   return f;
 }
 // Whether the waves of a workgroup share a row's span out, or have one each.  Own tokens of up to 100 / 400 / 1000 (whole calls, 8 K/V heads,
-// shared out against one each): 32 rows 31 / 34 us and 28 / 42, 64 rows 35 / 37 and 34 / 44, 128 rows 42 / 39 and 46 / 48, 256 rows 56 / 49, 70 / 69
-// and 121 / 132, 512 rows 90 / 74, 119 / 116 and 217 / 225; 8-bit pools, up to 200, 96 rows 41 / 40, 256 rows 61 / 49.
+// shared out against one each): 32 rows 32 / 33 us and 28 / 42, 64 rows 35 / 36 and 33 / 43, 128 rows 41 / 38 and 46 / 47, 256 rows 56 / 47, 70 / 67
+// and 118 / 129, 512 rows 89 / 73, 120 / 115 and 221 / 222; 8-bit pools, up to 200, 96 rows 41 / 40, 256 rows 59 / 48.
 bool rows_split(int batch, int n_kv_heads) { return (int64_t)batch * n_kv_heads < 1024; }
 int items_of(const SharedBatch& b, const Form& f) {
   return (int)((int64_t)b.batch * (b.n_q_heads / b.n_kv_heads) / f.columns) + b.n_groups + f.wanted;
@@ -107,7 +113,7 @@ __device__ __forceinline__ int last_not_above(const int32_t* at, int n, int v) {
 // Rows of length zero attend to nothing: what their tables hold is not looked at.
 // Bound: a chain of look-ups and barriers (a workgroup alone: 5 us), and the tables, which one CU reads at some 30 GB/s.  4 rows 7 us; 162 rows in
 // 24 groups, 250 pages 13 us (loads 3, comparison 3, groups' sums 3, prefix items 2, row items 2); 512 rows in one group 15 us.  A workgroup per
-// 8 / 16 / 32 / 64 rows, the whole call: 512 rows behind one prompt 140 / 140 / 142 / 146 us, 24 groups of 8 157 / 157 / 159 / 162, 256 rows 55 / 55 / 56 / 62.
+// 8 / 16 / 32 / 64 rows, the whole call: 512 rows behind one prompt 141 / 140 / 140 / 144 us, 24 groups of 8 155 / 154 / 154 / 158, 256 rows 56 / 56 / 57 / 62.
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArgs a) {
   constexpr int T = kPlanThreads;
   __shared__ int32_t s_starts[kPlanHeld + 1], s_tokens[kPlanHeld], s_group[4 * kPlanHeld], s_pages[T], s_first[T];
@@ -223,8 +229,8 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(const PlanArg
   auto tiles_of = [&](int g) { return ((end_of(g) - begin_of(g)) * (b.n_q_heads / b.n_kv_heads) + a.columns - 1) / a.columns; };
   for (int g = tid; g < n_groups; g += T) {
     int pages = common[g];
-    // A short prefix is left to the rows where one of them has more than the shortest span behind it: there is little to save, and a row
-    // has no more slots for partials than spans of that length.
+    // A short prefix is left to the rows where one of them has more than the shortest span behind it: a row has as many slots for partials as
+    // spans of that length, so that prefix and spans together could need one more than there are.
     if (last[g] <= first[g] || (pages < kMinSpanPages && longest[g] - pages * 16 > kDecodeSpanMin)) pages = 0;
     common[g] = pages;
     if (pages) atomicAdd(&work, (unsigned long long)tiles_of(g) * (unsigned long long)pages);
@@ -995,7 +1001,7 @@ int attn_prefix_items_most(int max_batch, int n_q_heads, int n_kv_heads) {
 }
 
 // Spans of what rows have behind their prefix: as in decode attention where four waves share one, shorter where each is a wave's (512 / 1024 /
-// 2048 tokens, 8 K/V heads: 256 rows of up to 400 tokens 78 / 69 / 69 us, 512 of up to 1000 259 / 225 / 225; 16 rows of 64 heads, up to 1000, 54 / 64 / 65).
+// 2048 tokens, 8 K/V heads: 256 rows of up to 400 tokens 72 / 68 / 68 us, 512 of up to 1000 255 / 221 / 215; two groups of 8 rows of 64 heads, up to 1000, 52 / 63 / 63).
 int attn_shared_span(int batch, int n_kv_heads) {
   return rows_split(batch, n_kv_heads) ? attn_decode_span(batch, n_kv_heads) : 1024;
 }

@@ -86,7 +86,7 @@ __device__ __forceinline__ double wave_sum_double(double v) {
 
 // KEEP: a thread has eight vectors at most and keeps them in registers; else the piece is read twice, and the tokens of threads whose
 // largest logit is among the wanted a third time.  Bound: reading, 512 rows of 32000 fp32 logits 18.3 us (65.5 MB, 3.6 TB/s with the beginning and
-// the end of two workgroups a CU), 528 of 152067 in bf16, a quarter of them finished, 39 us (120 MB, 3.1 TB/s): beside it a maximum, an exponential, an
+// the end of two workgroups a CU), 528 of 152067 in bf16, a quarter of them finished, 38 to 39 us (120 MB, 3.1 TB/s): beside it a maximum, an exponential, an
 // addition in 64 bits and a comparison to a logit.  (Terms added in fp32 per thread 17.9 and 36 us, in pairs 18.2 and 38; a sum so formed
 // is off by 2^-24 of what the likeliest token carries.)
 template <typename T, bool KEEP>
@@ -334,9 +334,9 @@ int fail_hip(hipError_t e, const char* what) {
 }
 
 // How a row is cut.  A few rows into enough pieces that they keep the chip busy, of some thousand logits at least (the second kernel ranks
-// candidates of every piece: 2 rows of 5 beams, 128256 logits, 31 / 25 pieces 14.8 / 12.3 us).  Many into pieces that the registers of a
-// workgroup of 1024 threads hold, as long as they are not too many; bf16, twice as many logits to a thread, of 512 (528 rows of 152067, 3
-// pieces 56 us, 5 of half the threads 49; fp32 70 and 83).
+// candidates of every piece: 2 groups of 5 beams, 128256 logits, 31 / 25 pieces 19.1 / 17.3 us, the caches emptied in front).  Many into
+// pieces that the registers of a workgroup of 1024 threads hold, as long as they are not too many; bf16, twice as many logits to a thread, of
+// 512 (528 rows of 152067, the pass of two inputs in turn: 3 pieces 48 us, 5 of half the threads 39; fp32, 5 pieces 58 us, 8 smaller ones 70).
 struct Cut {
   int pieces, threads;
 };
