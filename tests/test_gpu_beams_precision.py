@@ -58,13 +58,10 @@ def test_a_row_held_to_one_token_costs_nothing(n, masked, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("n", [2, 9, 1000, 33003, 200001])
-@pytest.mark.parametrize("tokens", [2, 3])
+@pytest.mark.parametrize("n,tokens", [(2, 2)] + [(n, tokens) for n in (9, 1000, 33003, 200001) for tokens in (2, 3)])
 def test_rows_that_differ_by_a_constant_are_equal(n, tokens, dtype):
     """Two or three tokens left, the same distances between their logits in every beam, the logits themselves anything: of equal candidates the lower
     beam comes first."""
-    if n < tokens:
-        pytest.skip("fewer tokens than are left")
     rng = np.random.default_rng(n + tokens)
     beams, apart = 10, [0.0, 0.5, 2.0][:tokens]
     at = np.sort(rng.permutation(n)[:tokens])
