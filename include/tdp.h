@@ -463,7 +463,7 @@ TDP_API int tdp_lm_head_logprobs(tdp_ends* e, const void* hidden_in, int32_t n_r
  * infinity or with nothing but minus infinity, which has no distribution); places behind the last have parent and token -1, score minus
  * infinity, finished_out 0.  The candidates are formed and compared in 64 bits, but for the exponentials, which are fp32 numbers relative to
  * the row's largest logit m: its own is exactly 1 (a row held to one token costs nothing), and ln sum is off by at most
- * 2^-23 sum_{z < m} p (1 + m - z), p the tokens' probabilities.
+ * 2^-23 sum_{z < m} p (1 + m - z) + n 2^-53, p the tokens' probabilities.
  *   logits   dev, TDP_F32 or TDP_BF16, [n_groups * beams][n], rows ld >= n elements apart, at any alignment of their type
  *   scores   dev fp32 [n_groups * beams]; the results overlap neither them nor one another (finished_out may be finished itself)
  *   finished dev int32 [n_groups * beams], not 0: finished; or null.  end_token: in [0, n), or, with finished null, -1: none

@@ -3,7 +3,8 @@
 A row's cost ln sum_j e^(z_j - m), m its largest logit, may be off by
   E = 2^-23 sum_{z_j < m} p_j (1 + m - z_j):
 a term is off by the roundings of z_j - m and of the exponent (2^-24 |z_j - m| each, relative) and by the exponential's 1 ulp, the largest's by nothing;
-everything behind the terms is in 64 bits (a few 2^-53 of a candidate).  Candidates further apart than the E of both have one order."""
+everything behind the terms is in 64 bits: n additions of 2^-53 of the sum, and a few 2^-53 of a candidate.  Candidates further apart than the E of
+both have one order."""
 import numpy as np
 
 
@@ -15,7 +16,7 @@ def bound(z, finished=None):
         p = np.exp(-below)
         e = 2.0 ** -23 * np.where(p > 0, p * (1 + below), 0.0)
     e[below == 0] = 0
-    e = e.sum(1) / p.sum(1)
+    e = e.sum(1) / p.sum(1) + z.shape[1] * 2.0 ** -53
     return e if finished is None else np.where(np.asarray(finished) != 0, 0.0, e)
 
 

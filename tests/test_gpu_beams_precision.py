@@ -94,3 +94,26 @@ def test_equal_logits_cost_the_logarithm_of_their_number(n, dtype):
             parent, token, score, _ = b.select(z, [-1.0, -0.5, -1.0], 3, 2)
         assert parent.tolist() == [[1, 1]] and token.tolist() == [[0, 1]]
         assert (score == np.float32(-0.5 - np.log(n))).all()
+
+
+def test_a_term_is_off_by_no_more_than_stated():
+    """Two tokens d apart: the likelier one's candidate is -ln(1 + e^-d), whose own rounding to fp32 (2^-24 of it) hides little of the term's error of
+    (1 + d) 2^-23 where d is large; and the bound as it stands where it is small."""
+    rng = np.random.default_rng(1)
+    rows = 1 << 16
+    d = np.concatenate([rng.uniform(0, 2, rows // 4), rng.uniform(2, 20, rows // 2), rng.uniform(20, 86, rows // 4)]).astype(np.float32)
+    top = rng.choice([0.0, 1.0, -5.5, 20.0], rows).astype(np.float32)
+    z = np.stack([top, top - d], 1)
+    with Beams(rows, 1) as b:
+        parent, token, score, _ = b.select(torch.from_numpy(z).cuda(), [0.0] * rows, 1, 1)
+    x = z.astype(np.float64)
+    apart = x[:, 0] - x[:, 1]
+    assert (apart > 0).sum() > rows - 10 and (token[apart > 0] == 0).all() and (parent[:, 0] == np.arange(rows)).all()
+    want = -np.log1p(np.exp(-apart))
+    off = np.abs(score[:, 0] - want)
+    # (in 64 bits: 1 + e^-d is rounded by 2^-53 of itself, 1 to 2, and its logarithm is that much off, whatever is left of it)
+    allowed = 2.0 ** -23 * (1 + apart) * np.exp(-apart) / (1 + np.exp(-apart)) + (2.0 ** -24 + 2.0 ** -50) * np.abs(want) + 2.0 ** -52
+    for low, high in ((0, 0.5), (0.5, 2), (2, 8), (8, 20), (20, 87)):
+        some = (apart >= low) & (apart < high)
+        print("%g to %g apart: at most %.2f of what is allowed" % (low, high, (off / allowed)[some].max()))
+    assert (off <= allowed).all()
